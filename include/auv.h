@@ -470,6 +470,117 @@ int64_t auv_shac_work_bytes(int32_t n_envs, int32_t h);
 int auv_shac_window(auv_env* env, const auv_shac_config* cfg, const auv_mlp* policy, const auv_mlp* value,
                     const auv_shac_buffers* out, float* grad_policy, float* stats, void* work, void* stream);
 
+/* ---- Network layers over rollouts ------------------------------------------------------
+ * Layers that a policy or critic uses around its matrix products: a gated linear recurrence
+ * over the steps of a rollout (a memory for what one observation does not show, cut where
+ * episodes end), group norm with an activation (one group and one position: layer norm), and
+ * dropout from the counter-based generator.  Each has its gradient.  Tensors are fp32 or bf16
+ * with strides in elements; sums, statistics and states are fp32, and a stored bf16 value is
+ * rounded once.  Sizes are >= 1.  Results are deterministic (same inputs, same bits).  Apart from what
+ * a function names, its outputs share no memory with its inputs or each other; halves of one wider
+ * buffer are separate tensors.  Pointers are aligned to their elements, `work` to 16 bytes.
+ * AUV_EINVAL, nothing enqueued: sizes below 1 or beyond the limits given, an unknown type, kind
+ * or activation, NULL or misaligned pointers, negative strides, an output whose elements share
+ * memory, an output at an input's address. */
+enum { AUV_FP32 = 0, AUV_BF16 = 1 };
+
+/* Gated linear recurrence.  Of n sequences with c channels each, from the state s_{-1} = h0:
+ *   AUV_SCAN_SIGMOID  f = sigma(gate), h_t = f s_{t-1} + (1 - f) x_t
+ *   AUV_SCAN_DECAY    f = gate,        h_t = f s_{t-1} + x_t
+ *   s_t = 0 where the episode ended at step t (done nonzero), else h_t
+ * Steps from a sequence's length on hold the state, h_t = s_t = s_{t-1}: their gate, input and
+ * done are not looked at.  Nothing before an episode's end reaches what is after it, also not as
+ * NaN.  The tensors may lie in any order ([T][n][c], [n][T][c], [c][T][n], parts of a wider
+ * buffer, broadcast inputs); they run fastest where c or n is the axis of stride 1 in all. */
+enum { AUV_SCAN_SIGMOID = 0, AUV_SCAN_DECAY = 1 };
+
+typedef struct {
+  void* p;
+  int64_t st, sn, sc; /* strides of the step, the sequence and the channel */
+} auv_seq;
+
+typedef struct {
+  float* p;       /* [n][c], fp32 */
+  int64_t sn, sc;
+} auv_seq_state;
+
+typedef struct {
+  int32_t T, n, c;      /* n c <= 2^30 */
+  int32_t type, kind;   /* AUV_FP32 or AUV_BF16; AUV_SCAN_* */
+  auv_seq gate, x;      /* inputs */
+  auv_seq h;            /* output of the forward pass, input of the backward pass */
+  const float* done;    /* [T][n] as auv_rollout records it, or NULL */
+  const int32_t* lens;  /* [n] steps of each sequence, below 0 as 0, above T as T; or NULL */
+  auv_seq_state h0;     /* p NULL: zero */
+  auv_seq_state last;   /* forward: s_{T-1}, or p NULL; may be the memory of h0 with the same strides */
+} auv_scan;
+
+typedef struct {
+  auv_seq dout;         /* gradient of h, p NULL: zero */
+  auv_seq_state dlast;  /* gradient of s_{T-1}, p NULL: zero */
+  auv_seq dgate, dx;    /* results; zero at held steps */
+  auv_seq_state dh0;    /* result, or p NULL */
+} auv_scan_grad;
+
+/* Bytes of device workspace of auv_scan_forward (g NULL) or auv_scan_backward on these tensors:
+ * 0 unless the columns are too few for the chip and the steps many (work may then be NULL); -1 on
+ * bad arguments. */
+int64_t auv_scan_work_bytes(const auv_scan* s, const auv_scan_grad* g);
+int auv_scan_forward(const auv_scan* s, void* work, void* stream);
+int auv_scan_backward(const auv_scan* s, const auv_scan_grad* g, void* work, void* stream);
+
+/* Dropout that stores no mask.  Element (row, channel) is drawn as 16 bits of the Philox block
+ * with key seed and counter (row0 + row, step, 3 | site << 8, channel / 8): half channel % 8, low
+ * halves of the words first; it is dropped where they are below `drop`, else kept and scaled by
+ * 65536 / (65536 - drop).  A gradient draws the same mask again.  row0: global number of the first
+ * row, so that results do not depend on how a batch is split. */
+typedef struct {
+  uint64_t seed;
+  uint32_t step;  /* update number */
+  uint32_t site;  /* layer, below 2^24 */
+  uint32_t row0;
+  uint32_t drop;  /* probability in 65536ths, below 65536 */
+} auv_drop;
+
+/* Channels-last tensor [n][s][c] of stride 1 over c: row (i, j) starts at p + i sn + j ss.  Rows are
+ * numbered i s + j for dropout. */
+typedef struct {
+  void* p;
+  int64_t sn, ss;
+} auv_rows;
+
+/* y = dropout(x) (+ add, unless p NULL).  y may be x or add itself.  n s <= 2^32 - row0, c <= 2^30. */
+int auv_dropout(const auv_drop* drop, int32_t type, int32_t n, int32_t s, int32_t c, const auv_rows* x,
+                const auv_rows* add, const auv_rows* y, void* stream);
+
+/* Group norm over the s positions and c / groups channels of each group of each sample, with an
+ * activation: xhat = (x - mean) rstd, rstd = 1 / sqrt(var + eps), y = act(weight xhat + bias).
+ * With `drop`, x is dropout(x). */
+enum { AUV_ACTIVATION_NONE = 0, AUV_ACTIVATION_RELU = 1, AUV_ACTIVATION_SILU = 2, AUV_ACTIVATION_TANH = 3 };
+
+typedef struct {
+  int32_t n, s, c, groups; /* groups divides c; n s c <= 2^40, c <= 2^20, n s and n groups < 2^31, n groups < 2^24
+                              for groups of more than 1024 numbers or of several groups and positions */
+  int32_t type, act;
+  float eps;               /* >= 0 */
+  auv_rows x;
+  const float *weight, *bias; /* [c] or NULL (1 and 0) */
+  float *mean, *rstd;      /* [n][groups]: results of the forward pass, inputs of the backward pass */
+  const auv_drop* drop;    /* host memory, or NULL */
+} auv_norm;
+
+typedef struct {
+  auv_rows dout;            /* gradient of y */
+  auv_rows dx;              /* result */
+  float *dweight, *dbias;   /* [c] results, or NULL */
+} auv_norm_grad;
+
+/* Bytes of device workspace of auv_norm_forward (backward 0) or auv_norm_backward (1) for these
+ * sizes (-1 on bad arguments); work may be NULL where it is 0. */
+int64_t auv_norm_work_bytes(const auv_norm* d, int32_t backward);
+int auv_norm_forward(const auv_norm* d, const auv_rows* y, void* work, void* stream);
+int auv_norm_backward(const auv_norm* d, const auv_norm_grad* g, void* work, void* stream);
+
 /* Message for the calling thread's last error ("" if none). */
 const char* auv_last_error(void);
 

@@ -27,8 +27,10 @@ Modules
   shac      the SHAC actor objective over a short window of the paper task and its
             gradient through the policy, reward, observation, RK4 + Fossen and the
             terminal value (torch autograd on float64 tensors)
+  layers    the network layers over rollouts: gated recurrence, group norm with an activation,
+            dropout's draws, and their gradients
 
 Every function is pinned by a ``-m "not gpu"`` test against closed forms, invariants,
 special cases or an independent library; see the test files under ``tests/``.
 """
-from . import rng, dynamics, fluid, mlp, gae, env, ppo, paper_task, shac  # noqa: F401
+from . import rng, dynamics, fluid, mlp, gae, env, ppo, paper_task, shac, layers  # noqa: F401

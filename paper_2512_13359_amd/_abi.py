@@ -23,6 +23,9 @@ AUV_FLUID_FOSSEN, AUV_FLUID_INERTIA_BOX = 0, 1
 AUV_STATIC_STATS_FLOATS = 2 * 1024 * 1024
 AUV_CONV_UNIFORM, AUV_CONV_UNIFORM_OPEN0, AUV_CONV_AFFINE, AUV_CONV_BF16 = 0, 1, 2, 3
 AUV_PROBE_EXP, AUV_PROBE_RCP, AUV_PROBE_FMA, AUV_PROBE_MFMA_BF16 = 0, 1, 2, 3
+AUV_FP32, AUV_BF16 = 0, 1
+AUV_SCAN_SIGMOID, AUV_SCAN_DECAY = 0, 1
+AUV_ACTIVATION_NONE, AUV_ACTIVATION_RELU, AUV_ACTIVATION_SILU, AUV_ACTIVATION_TANH = 0, 1, 2, 3
 OBS_DIM, ACT_DIM, STATE_DIM, PARAM_DIM, HIDDEN, ENVS_PER_GROUP = 23, 8, 13, 24, 256, 64
 
 _f = ctypes.c_float
@@ -84,6 +87,43 @@ class AuvShacBuffers(ctypes.Structure):
                                    "grad_state0")]
 
 
+# The layers' structures with their nested tensors' fields in line (the same layout).
+def _seq(name):
+    return [(name, _vp)] + [(f"{name}_{k}", ctypes.c_int64) for k in ("st", "sn", "sc")]
+
+
+def _seq_state(name):
+    return [(name, _vp)] + [(f"{name}_{k}", ctypes.c_int64) for k in ("sn", "sc")]
+
+
+class AuvScan(ctypes.Structure):
+    _fields_ = [(k, ctypes.c_int32) for k in ("T", "n", "c", "type", "kind")] + [
+        *_seq("gate"), *_seq("x"), *_seq("h"), ("done", _vp), ("lens", _vp), *_seq_state("h0"), *_seq_state("last")]
+
+
+class AuvScanGrad(ctypes.Structure):
+    _fields_ = [*_seq("dout"), *_seq_state("dlast"), *_seq("dgate"), *_seq("dx"), *_seq_state("dh0")]
+
+
+class AuvDrop(ctypes.Structure):
+    _fields_ = [("seed", ctypes.c_uint64)] + [(k, ctypes.c_uint32) for k in ("step", "site", "row0", "drop")]
+
+
+class AuvRows(ctypes.Structure):
+    _fields_ = [("p", _vp), ("sn", ctypes.c_int64), ("ss", ctypes.c_int64)]
+
+
+class AuvNorm(ctypes.Structure):
+    _fields_ = [(k, ctypes.c_int32) for k in ("n", "s", "c", "groups", "type", "act")] + [
+        ("eps", _f), ("x", _vp), ("x_sn", ctypes.c_int64), ("x_ss", ctypes.c_int64)] + [
+        (k, _vp) for k in ("weight", "bias", "mean", "rstd", "drop")]
+
+
+class AuvNormGrad(ctypes.Structure):
+    _fields_ = [("dout", _vp), ("dout_sn", ctypes.c_int64), ("dout_ss", ctypes.c_int64),
+                ("dx", _vp), ("dx_sn", ctypes.c_int64), ("dx_ss", ctypes.c_int64), ("dweight", _vp), ("dbias", _vp)]
+
+
 def ppo_nw(n_out: int) -> int:
     """AUV_PPO_NW: packed offset of b1 (the weight matrices' length)."""
     return 256 * 23 + 256 * 256 + n_out * 256
@@ -133,6 +173,13 @@ def _load() -> ctypes.CDLL:
         "auv_shac_work_bytes": (i64, [i32, i32]),
         "auv_shac_window": (ctypes.c_int, [_vp, P(AuvShacConfig), P(AuvMlp), P(AuvMlp), P(AuvShacBuffers), _vp, _vp,
                                            _vp, _vp]),
+        "auv_scan_work_bytes": (i64, [P(AuvScan), P(AuvScanGrad)]),
+        "auv_scan_forward": (ctypes.c_int, [P(AuvScan), _vp, _vp]),
+        "auv_scan_backward": (ctypes.c_int, [P(AuvScan), P(AuvScanGrad), _vp, _vp]),
+        "auv_dropout": (ctypes.c_int, [P(AuvDrop), i32, i32, i32, i32, P(AuvRows), P(AuvRows), P(AuvRows), _vp]),
+        "auv_norm_work_bytes": (i64, [P(AuvNorm), i32]),
+        "auv_norm_forward": (ctypes.c_int, [P(AuvNorm), P(AuvRows), _vp, _vp]),
+        "auv_norm_backward": (ctypes.c_int, [P(AuvNorm), P(AuvNormGrad), _vp, _vp]),
         "auv_last_error": (ctypes.c_char_p, []),
     }
     for name, (res, args) in sig.items():
@@ -152,6 +199,9 @@ def _check(rc: int) -> None:
 def ptr(t) -> int | None:
     """Device address of a tensor (None for None)."""
     return None if t is None else t.data_ptr()
+
+
+address = ctypes.addressof   # host address of a structure
 
 
 def stream_ptr(stream=None) -> int | None:
@@ -288,6 +338,41 @@ def auv_shac_window(h: int, cfg: AuvShacConfig, policy: AuvMlp | None, value: Au
                                stream_ptr(stream)))
 
 
+def _work_bytes(n: int) -> int:
+    if n < 0:
+        _check(AUV_EINVAL)
+    return n
+
+
+def auv_scan_work_bytes(s: AuvScan, g: AuvScanGrad | None = None) -> int:
+    return _work_bytes(lib.auv_scan_work_bytes(s, g))
+
+
+def auv_scan_forward(s: AuvScan, work, stream=None) -> None:
+    _check(lib.auv_scan_forward(s, ptr(work), stream_ptr(stream)))
+
+
+def auv_scan_backward(s: AuvScan, g: AuvScanGrad, work, stream=None) -> None:
+    _check(lib.auv_scan_backward(s, g, ptr(work), stream_ptr(stream)))
+
+
+def auv_dropout(drop: AuvDrop, dtype: int, n: int, s: int, c: int, x: AuvRows, add: AuvRows | None, y: AuvRows,
+                stream=None) -> None:
+    _check(lib.auv_dropout(drop, dtype, n, s, c, x, add, y, stream_ptr(stream)))
+
+
+def auv_norm_work_bytes(d: AuvNorm, backward: bool) -> int:
+    return _work_bytes(lib.auv_norm_work_bytes(d, backward))
+
+
+def auv_norm_forward(d: AuvNorm, y: AuvRows, work, stream=None) -> None:
+    _check(lib.auv_norm_forward(d, y, ptr(work), stream_ptr(stream)))
+
+
+def auv_norm_backward(d: AuvNorm, g: AuvNormGrad, work, stream=None) -> None:
+    _check(lib.auv_norm_backward(d, g, ptr(work), stream_ptr(stream)))
+
+
 def auv_last_error() -> str:
     return lib.auv_last_error().decode()
 
@@ -345,6 +430,17 @@ def make_shac_config(h: int, mode: int, gamma: float, max_grad_norm: float = 0.0
 
 def make_shac_buffers(**kw) -> AuvShacBuffers:
     return AuvShacBuffers(**{k: ptr(v) for k, v in kw.items()})
+
+
+def make_drop(p: float, seed: int, step: int = 0, site: int = 0, row0: int = 0) -> AuvDrop:
+    """Dropout with probability p (rounded to 65536ths): the draws of update `step` and layer `site`
+    (below 2^24) under a 64-bit seed; row0: global number of the tensors' first row."""
+    if not 0.0 <= p < 1.0 or round(p * 65536) >= 65536:
+        raise AuvError(AUV_EINVAL, f"make_drop: p must be in [0, 1) and below 1 in 65536ths, got {p}")
+    for name, v, bits in (("seed", seed, 64), ("step", step, 32), ("site", site, 24), ("row0", row0, 32)):
+        if not 0 <= v < 1 << bits:
+            raise AuvError(AUV_EINVAL, f"make_drop: {name} must be in [0, 2^{bits}), got {v}")
+    return AuvDrop(seed, step, site, row0, round(p * 65536))
 
 
 def make_rollout_buffers(**kw) -> AuvRolloutBuffers:

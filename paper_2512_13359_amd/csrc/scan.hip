@@ -1,0 +1,393 @@
+// Gated linear recurrence, forward (kernels and C interface; scan_backward.hip: its gradient).
+//   sigmoid: f = sigma(gate), h_t = f s_{t-1} + (1 - f) x_t     decay: f = gate, h_t = f s_{t-1} + x_t
+//   s_t = 0 where the episode ended at step t, else h_t; steps from a sequence's length on hold
+//   the state (h_t = s_t = s_{t-1}; their gate, input and done are not looked at).
+#include <algorithm>
+#include <cmath>
+
+#include "scan.hpp"
+
+namespace auv {
+
+// f and the input's share of U steps from t0 on; steps from tend on hold the state
+template <class T, int V, int U, bool SIG, bool MASK, bool NI>
+struct ForwardSteps {
+  Vec<T, V> z[U], x[U];
+  typename Columns<V, NI>::Flags d[MASK ? U : 1];
+
+  __device__ __forceinline__ void load(const ScanArgs& a, const Columns<V, NI>& col, const T* gate, const T* in, int t0,
+                                       int tend) {
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      if (t0 + u < tend) {
+        z[u].load(gate + (int64_t)(t0 + u) * a.gate.st);
+        x[u].load(in + (int64_t)(t0 + u) * a.x.st);
+        if constexpr (MASK)
+          if (a.done) d[u] = col.load_done(a, t0 + u);
+      }
+    }
+  }
+  __device__ __forceinline__ void masks(const ScanArgs& a, const Columns<V, NI>& col,
+                                        const typename Columns<V, NI>::Lens& len, int u, int t, uint32_t& done,
+                                        uint32_t& hold) const {
+    hold = col.over(len, t);
+    done = a.done ? col.ended(d[u]) & ~hold : 0u;
+  }
+  __device__ __forceinline__ void step(int u, int k, uint32_t hold, float& f, float& in) const {
+    const float zz = z[u].get(k), xx = x[u].get(k);
+    if constexpr (SIG) {
+      float g;
+      sigmoid2<T>(zz, f, g);
+      in = g * xx;
+    } else {
+      f = zz;
+      in = xx;
+    }
+    if (MASK && (hold >> k & 1u)) {
+      f = 1.0f;
+      in = 0.0f;
+    }
+  }
+};
+
+// (P, S) of every chunk of steps but the last: each wave runs a contiguous part of its chunk, the
+// first wave joins the parts.
+template <class T, int V, bool SIG, bool MASK, bool NI>
+__global__ __launch_bounds__(1024) void k_scan_ranges(ScanArgs a) {
+  constexpr int U = scan_steps<V>();
+  extern __shared__ float lds[];   // [W][V][2][64]
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), W = blockDim.x >> 6;
+  const Columns<V, NI> col(a, blockIdx.x, lane);
+  const T *gate = col.template base<T>(a.gate), *in = col.template base<T>(a.x);
+  typename Columns<V, NI>::Lens len{};
+  if constexpr (MASK) len = col.load_lens(a);
+  const int part = a.chunk / W, tb = blockIdx.y * a.chunk + wave * part, te = min(a.T, tb + part);
+  float P[V], S[V];
+#pragma unroll
+  for (int k = 0; k < V; ++k) P[k] = 1.0f, S[k] = 0.0f;
+  uint32_t cut = 0;
+  for (int t0 = tb; t0 < te; t0 += U) {
+    ForwardSteps<T, V, U, SIG, MASK, NI> st;
+    st.load(a, col, gate, in, t0, te);
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      if (t0 + u < te) {
+        uint32_t done = 0, hold = 0;
+        if constexpr (MASK) st.masks(a, col, len, u, t0 + u, done, hold);
+#pragma unroll
+        for (int k = 0; k < V; ++k) {
+          float f, v;
+          st.step(u, k, hold, f, v);
+          P[k] *= f;
+          S[k] = __builtin_fmaf(f, S[k], v);
+          if (MASK && (done >> k & 1u)) P[k] = 1.0f, S[k] = 0.0f;
+        }
+        cut |= done;
+      }
+    }
+  }
+  mark_cut<V>(P, cut);
+  put_range<V>(lds + wave * 128 * V, lane, P, S);
+  __syncthreads();
+  if (wave) return;
+  for (int w = 1; w < W; ++w) join_range<V>(lds + w * 128 * V, lane, P, S);
+  put_range<V>(a.agg + ((int64_t)blockIdx.y * a.tiles + blockIdx.x) * 128 * V, lane, P, S);
+}
+
+template <class T, int V, bool SIG, bool MASK, bool NI>
+__global__ __launch_bounds__(1024) void k_scan_forward(ScanArgs a) {
+  constexpr int U = scan_steps<V>();
+  extern __shared__ float lds[];   // [2][W][V][2][64], by round parity
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), W = blockDim.x >> 6;
+  const Columns<V, NI> col(a, blockIdx.x, lane);
+  const T *gate = col.template base<T>(a.gate), *in = col.template base<T>(a.x);
+  T* out = col.template base<T>(a.h);
+  typename Columns<V, NI>::Lens len{};
+  if constexpr (MASK) len = col.load_lens(a);
+  const int tb = blockIdx.y * a.chunk, te = min(a.T, tb + a.chunk);
+
+  float s[V];
+#pragma unroll
+  for (int k = 0; k < V; ++k) s[k] = a.h0.p ? a.h0.p[col.state_at(a, a.h0, k)] : 0.0f;
+  if (blockIdx.y) {   // the chunks before this one, a part per wave
+    float P[V], S[V];
+#pragma unroll
+    for (int k = 0; k < V; ++k) P[k] = 1.0f, S[k] = 0.0f;
+    const int j1 = (int)((int64_t)(wave + 1) * blockIdx.y / W);
+    for (int j = (int)((int64_t)wave * blockIdx.y / W); j < j1; ++j)
+      join_range<V>(a.agg + ((int64_t)j * a.tiles + blockIdx.x) * 128 * V, lane, P, S);
+    put_range<V>(lds + (W + wave) * 128 * V, lane, P, S);
+    __syncthreads();
+    for (int w = 0; w < W; ++w) run_range<V>(lds + (W + w) * 128 * V, lane, s);
+  }
+
+  int parity = 0;
+  for (int r0 = tb; r0 < te; r0 += W * U, parity ^= 1) {
+    const int t0 = r0 + wave * U;
+    ForwardSteps<T, V, U, SIG, MASK, NI> st;
+    st.load(a, col, gate, in, t0, te);
+    float f[U][V], v[U][V];
+    uint32_t done[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      done[u] = 0;
+      if (t0 + u < te) {
+        uint32_t hold = 0;
+        if constexpr (MASK) st.masks(a, col, len, u, t0 + u, done[u], hold);
+#pragma unroll
+        for (int k = 0; k < V; ++k) st.step(u, k, hold, f[u][k], v[u][k]);
+      } else {
+#pragma unroll
+        for (int k = 0; k < V; ++k) f[u][k] = 1.0f, v[u][k] = 0.0f;
+      }
+    }
+    float end[V];   // the state after the round
+    if (W > 1) {
+      float P[V], S[V];
+      uint32_t cut = 0;
+#pragma unroll
+      for (int k = 0; k < V; ++k) P[k] = 1.0f, S[k] = 0.0f;
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+#pragma unroll
+        for (int k = 0; k < V; ++k) {
+          P[k] *= f[u][k];
+          S[k] = __builtin_fmaf(f[u][k], S[k], v[u][k]);
+          if (MASK && (done[u] >> k & 1u)) P[k] = 1.0f, S[k] = 0.0f;
+        }
+        cut |= done[u];
+      }
+      mark_cut<V>(P, cut);
+      float* x = lds + parity * W * 128 * V;
+      put_range<V>(x + wave * 128 * V, lane, P, S);
+      __syncthreads();
+      for (int w = 0; w < wave; ++w) run_range<V>(x + w * 128 * V, lane, s);
+#pragma unroll
+      for (int k = 0; k < V; ++k) end[k] = s[k];
+      for (int w = wave; w < W; ++w) run_range<V>(x + w * 128 * V, lane, end);
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      if (t0 + u < te) {
+        float h[V];
+#pragma unroll
+        for (int k = 0; k < V; ++k) {
+          h[k] = __builtin_fmaf(f[u][k], s[k], v[u][k]);
+          s[k] = MASK && (done[u] >> k & 1u) ? 0.0f : h[k];
+        }
+        if (col.active) store_own<T, V>(out + (int64_t)(t0 + u) * a.h.st, h, col.shift);
+      }
+    }
+    if (W > 1) {
+#pragma unroll
+      for (int k = 0; k < V; ++k) s[k] = end[k];
+    }
+  }
+  if (a.last.p && blockIdx.y == gridDim.y - 1 && wave == 0 && col.active) {
+#pragma unroll
+    for (int k = 0; k < V; ++k)
+      if (k >= col.shift) a.last.p[col.state_at(a, a.last, k)] = s[k];
+  }
+}
+
+int launch_scan_forward(const ScanArgs& a, const ScanShape& sh, bool bf16, bool sig, hipStream_t s) {
+  const bool mask = a.done || a.lens;
+  ScanArgs arg = a;
+  void* args[1] = {&arg};
+  const size_t range = sizeof(float) * 128 * sh.V;
+  if (sh.K > 1)
+    if (int rc = launch_kernel("auv_scan_forward", AUV_SCAN_KERNEL(k_scan_ranges), dim3(a.tiles, sh.K - 1), dim3(64 * sh.W), args,
+                               sh.W * range, s))
+      return rc;
+  return launch_kernel("auv_scan_forward", AUV_SCAN_KERNEL(k_scan_forward), dim3(a.tiles, sh.K), dim3(64 * sh.W), args,
+                       2 * sh.W * range, s);
+}
+
+// ----------------------------------------------------------------------- shapes -------
+
+// Whether no two elements of an output share memory: each axis steps over all of the ones inside it.
+static bool disjoint(const int64_t* stride, const int64_t* size, int n) {
+  int order[3] = {0, 1, 2};
+  std::sort(order, order + n, [&](int i, int j) { return stride[i] < stride[j]; });
+  int64_t span = 1;
+  for (int q = 0; q < n; ++q) {
+    const int i = order[q];
+    if (size[i] == 1) continue;
+    if (stride[i] < span) return false;
+    span = stride[i] * (size[i] - 1) + span;
+  }
+  return true;
+}
+
+static int check_state(const char* fn, const char* name, const auv_seq_state& s, const auv_scan* d, bool output) {
+  if (!s.p) return AUV_OK;
+  if (reinterpret_cast<uintptr_t>(s.p) & 3u) return set_error(AUV_EINVAL, "%s: '%s' is not 4-byte aligned", fn, name);
+  const int64_t st[2] = {s.sn, s.sc}, size[2] = {d->n, d->c};
+  for (int k = 0; k < 2; ++k)
+    if (st[k] < 0 || st[k] > ((int64_t)1 << 40)) return set_error(AUV_EINVAL, "%s: '%s' has a stride outside [0, 2^40]", fn, name);
+  if (output && !disjoint(st, size, 2)) return set_error(AUV_EINVAL, "%s: elements of '%s' share memory", fn, name);
+  return AUV_OK;
+}
+
+static int check_seq(const char* fn, const char* name, const auv_seq& s, const auv_scan* d, bool output) {
+  if (!s.p) return set_error(AUV_EINVAL, "%s: '%s' is NULL", fn, name);
+  if (reinterpret_cast<uintptr_t>(s.p) & (d->type == AUV_BF16 ? 1u : 3u))
+    return set_error(AUV_EINVAL, "%s: '%s' is not aligned to its elements", fn, name);
+  const int64_t st[3] = {s.st, s.sn, s.sc}, size[3] = {d->T, d->n, d->c};
+  for (int k = 0; k < 3; ++k)
+    if (st[k] < 0 || (size[k] - 1) * (st[k] >> 20) > ((int64_t)1 << 24))
+      return set_error(AUV_EINVAL, "%s: '%s' has a negative stride or spans 2^44 elements or more", fn, name);
+  if (output && !disjoint(st, size, 3)) return set_error(AUV_EINVAL, "%s: elements of '%s' share memory", fn, name);
+  return AUV_OK;
+}
+
+static int check_scan(const char* fn, const auv_scan* d) {
+  if (!d) return set_error(AUV_EINVAL, "%s: NULL argument", fn);
+  if (d->T < 1 || d->n < 1 || d->c < 1) return set_error(AUV_EINVAL, "%s: T, n and c must be >= 1", fn);
+  if ((int64_t)d->n * d->c > ((int64_t)1 << 30)) return set_error(AUV_EINVAL, "%s: n c exceeds 2^30", fn);
+  if (d->T > (1 << 30)) return set_error(AUV_EINVAL, "%s: T exceeds 2^30", fn);
+  if (d->type != AUV_FP32 && d->type != AUV_BF16) return set_error(AUV_EINVAL, "%s: unknown type %d", fn, d->type);
+  if (d->kind != AUV_SCAN_SIGMOID && d->kind != AUV_SCAN_DECAY) return set_error(AUV_EINVAL, "%s: unknown kind %d", fn, d->kind);
+  if ((reinterpret_cast<uintptr_t>(d->done) | reinterpret_cast<uintptr_t>(d->lens)) & 3u)
+    return set_error(AUV_EINVAL, "%s: 'done' or 'lens' is not 4-byte aligned", fn);
+  return AUV_OK;
+}
+
+static SeqTensor inner_first(const auv_seq& s, bool ni) {
+  return {static_cast<char*>(s.p), ni ? s.sc : s.sn, ni ? s.sn : s.sc, s.st};
+}
+
+// Columns, vectors, waves per workgroup and chunks for the tensors of one pass.
+static void scan_shape(const auv_scan* d, const auv_seq* const* seqs, int count, ScanArgs& a, ScanShape& sh) {
+  const int n = d->n, c = d->c;
+  bool unit_c = true, unit_n = true, rows = true;
+  for (int k = 0; k < count; ++k) {
+    unit_c &= c == 1 || seqs[k]->sc == 1;
+    unit_n &= n == 1 || seqs[k]->sn == 1;
+    rows &= n == 1 || seqs[k]->sn == c;
+  }
+  // the axis that is contiguous in every tensor; with none, the shorter stride, element by element
+  sh.ni = (unit_c && unit_n) ? c == 1 : (unit_c || unit_n) ? unit_n : d->x.sn < d->x.sc;
+  const bool unit = unit_c || unit_n, flat = !sh.ni && unit_c && rows;
+  a.Li = sh.ni ? n : (flat ? n * c : c);
+  a.Lo = sh.ni ? c : (flat ? 1 : n);
+  const int full = d->type == AUV_BF16 ? 8 : 4, cus = compute_units();
+  auto tiles_of = [&](int V) { return (int)(((int64_t)a.Lo * ((a.Li + V - 1) / V) + 63) / 64); };
+  // A vector that straddles sequences straddles two at most.
+  auto fits = [&](int V) { return unit && a.Li >= V && (sh.ni || c >= V || a.Li == c); };
+  sh.V = fits(full) ? full : 1;
+  if (sh.V == 1 && full == 8 && fits(2)) sh.V = 2;
+  if (sh.V == full && tiles_of(full) < cus / 2) sh.V = full == 8 ? 2 : 1;
+  a.nvec = (a.Li + sh.V - 1) / sh.V;
+  a.tiles = tiles_of(sh.V);
+  const int U = sh.V == 8 ? 4 : 8, most = sh.V == 8 ? 8 : 16;   // 64 KB of LDS at most
+  sh.W = 1;
+  while (sh.W < most && (int64_t)a.tiles * sh.W < 8 * cus && sh.W * U < d->T) sh.W *= 2;
+  const int span = sh.W * U, rounds = (d->T - 1) / span + 1;
+  sh.K = 1;
+  const bool in_place = d->last.p && d->last.p == d->h0.p;   // its chunks would read what the last one writes
+  if (sh.W == most && rounds >= 8 && a.tiles < cus && !in_place) sh.K = std::min((2 * cus - 1) / a.tiles + 1, rounds / 2);
+  a.chunk = ((rounds - 1) / sh.K + 1) * span;
+  sh.K = (d->T - 1) / a.chunk + 1;
+  a.K = sh.K;
+  a.T = d->T;
+  a.n = n;
+  a.c = c;
+  a.done = d->done;
+  a.lens = d->lens;
+}
+
+static void forward_args(const auv_scan* d, ScanArgs& a, ScanShape& sh) {
+  const auv_seq* seqs[3] = {&d->gate, &d->x, &d->h};
+  scan_shape(d, seqs, 3, a, sh);
+  a.gate = inner_first(d->gate, sh.ni);
+  a.x = inner_first(d->x, sh.ni);
+  a.h = inner_first(d->h, sh.ni);
+}
+
+static void backward_args(const auv_scan* d, const auv_scan_grad* g, ScanArgs& a, ScanShape& sh) {
+  const auv_seq* seqs[6] = {&d->gate, &d->h, &g->dgate, &g->dx, &d->x, &g->dout};
+  int count = 5;
+  if (g->dout.p) seqs[count++] = &g->dout;
+  scan_shape(d, seqs, count, a, sh);
+  a.gate = inner_first(d->gate, sh.ni);
+  a.x = inner_first(d->x, sh.ni);
+  a.h = inner_first(d->h, sh.ni);
+  a.dout = inner_first(g->dout, sh.ni);
+  a.dgate = inner_first(g->dgate, sh.ni);
+  a.dx = inner_first(g->dx, sh.ni);
+}
+
+static int64_t ranges_bytes(const ScanArgs& a, const ScanShape& sh) {
+  return sh.K > 1 ? (int64_t)sh.K * a.tiles * 128 * sh.V * sizeof(float) : 0;
+}
+
+}  // namespace auv
+
+// ------------------------------------------------------------------ C interface ----
+using namespace auv;
+
+extern "C" {
+
+int64_t auv_scan_work_bytes(const auv_scan* d, const auv_scan_grad* g) {
+  if (check_scan("auv_scan_work_bytes", d)) return -1;
+  ScanArgs a{};
+  ScanShape sh{};
+  if (g) backward_args(d, g, a, sh);
+  else forward_args(d, a, sh);
+  return ranges_bytes(a, sh);
+}
+
+int auv_scan_forward(const auv_scan* d, void* work, void* stream) {
+  const char* fn = "auv_scan_forward";
+  if (int rc = check_scan(fn, d)) return rc;
+  if (int rc = check_seq(fn, "gate", d->gate, d, false)) return rc;
+  if (int rc = check_seq(fn, "x", d->x, d, false)) return rc;
+  if (int rc = check_seq(fn, "h", d->h, d, true)) return rc;
+  if (d->h.p == d->gate.p || d->h.p == d->x.p) return set_error(AUV_EINVAL, "%s: 'h' is an input's memory", fn);
+  if (int rc = check_state(fn, "h0", d->h0, d, false)) return rc;
+  if (int rc = check_state(fn, "last", d->last, d, true)) return rc;
+  if (d->last.p && d->last.p == d->h0.p && (d->last.sn != d->h0.sn || d->last.sc != d->h0.sc))
+    return set_error(AUV_EINVAL, "%s: 'last' is the memory of 'h0' with other strides", fn);
+  ScanArgs a{};
+  ScanShape sh{};
+  forward_args(d, a, sh);
+  if (sh.K > 1 && (!work || !aligned16(work))) return set_error(AUV_EINVAL, "%s: 'work' is NULL or not 16-byte aligned", fn);
+  a.h0 = {d->h0.p, d->h0.sn, d->h0.sc};
+  a.last = {d->last.p, d->last.sn, d->last.sc};
+  a.agg = static_cast<float*>(work);
+  return launch_scan_forward(a, sh, d->type == AUV_BF16, d->kind == AUV_SCAN_SIGMOID, (hipStream_t)stream);
+}
+
+int auv_scan_backward(const auv_scan* d, const auv_scan_grad* g, void* work, void* stream) {
+  const char* fn = "auv_scan_backward";
+  if (int rc = check_scan(fn, d)) return rc;
+  if (!g) return set_error(AUV_EINVAL, "%s: NULL argument", fn);
+  if (int rc = check_seq(fn, "gate", d->gate, d, false)) return rc;
+  if (int rc = check_seq(fn, "x", d->x, d, false)) return rc;
+  if (int rc = check_seq(fn, "h", d->h, d, false)) return rc;
+  if (g->dout.p)
+    if (int rc = check_seq(fn, "dout", g->dout, d, false)) return rc;
+  if (int rc = check_seq(fn, "dgate", g->dgate, d, true)) return rc;
+  if (int rc = check_seq(fn, "dx", g->dx, d, true)) return rc;
+  const void* in[4] = {d->gate.p, d->x.p, d->h.p, g->dout.p};
+  for (const void* p : in)
+    if (g->dgate.p == p || g->dx.p == p) return set_error(AUV_EINVAL, "%s: 'dgate' or 'dx' is an input's memory", fn);
+  if (g->dgate.p == g->dx.p) return set_error(AUV_EINVAL, "%s: 'dgate' and 'dx' are the same memory", fn);
+  if (int rc = check_state(fn, "h0", d->h0, d, false)) return rc;
+  if (int rc = check_state(fn, "dlast", g->dlast, d, false)) return rc;
+  if (int rc = check_state(fn, "dh0", g->dh0, d, true)) return rc;
+  if (g->dh0.p && (g->dh0.p == d->h0.p || g->dh0.p == g->dlast.p))
+    return set_error(AUV_EINVAL, "%s: 'dh0' is an input's memory", fn);
+  ScanArgs a{};
+  ScanShape sh{};
+  backward_args(d, g, a, sh);
+  if (sh.K > 1 && (!work || !aligned16(work))) return set_error(AUV_EINVAL, "%s: 'work' is NULL or not 16-byte aligned", fn);
+  a.h0 = {d->h0.p, d->h0.sn, d->h0.sc};
+  a.last = {g->dlast.p, g->dlast.sn, g->dlast.sc};
+  a.dh0 = {g->dh0.p, g->dh0.sn, g->dh0.sc};
+  a.agg = static_cast<float*>(work);
+  return launch_scan_backward(a, sh, d->type == AUV_BF16, d->kind == AUV_SCAN_SIGMOID, (hipStream_t)stream);
+}
+
+}  // extern "C"

@@ -1,0 +1,186 @@
+// The gated linear recurrence over a rollout's steps: what its forward and backward kernels
+// share (layout of the columns, masks, the composition of step ranges) and their launch shapes.
+//
+// A column is one (sequence, channel); a range of its steps maps the state before it to the state
+// after it by s' = P s + S.  Ranges compose associatively, so a workgroup's W waves take U steps
+// each of the same 64 V columns, exchange (P, S) through LDS and redo their steps from the true
+// state with the inputs still in registers: every element is read once.  Where the columns are too few
+// to fill the chip the steps are split over K workgroups as well, whose (P, S) a first launch
+// leaves in the caller's workspace.
+//
+// P = 0 stands for a cut (an episode's end) and nothing else: what was before a cut must not reach
+// what is after it, be it NaN or infinite.  A product that underflows keeps the smallest denormal.
+#pragma once
+
+#include "auv_internal.hpp"
+#include "layers.hpp"
+
+namespace auv {
+
+struct SeqTensor {
+  char* p;
+  int64_t so, si, st;   // strides of the outer, inner and time axes, elements
+};
+struct SeqState {
+  float* p;
+  int64_t sn, sc;
+};
+
+struct ScanArgs {
+  SeqTensor gate, x, h, dout, dgate, dx;
+  SeqState h0, last;     // backward: last is the gradient of the last state, dh0 the result
+  SeqState dh0;
+  const float* done;     // [T][n] or null
+  const int32_t* lens;   // [n] or null
+  float* agg;            // [K][tiles][V][2][64]
+  int T, n, c;
+  int Li, Lo;            // columns as [Lo][Li]; Li is the axis of unit stride
+  int nvec;              // vectors per row of Li
+  int chunk;             // steps per workgroup, a multiple of W U (of U in the first launch)
+  int K, tiles;
+};
+
+__device__ __forceinline__ float smallest() { return __uint_as_float(1u); }
+
+// P2 P1 where zero stands for a cut only
+__device__ __forceinline__ float chain(float P2, float P1) {
+  const float p = P2 * P1;
+  return p == 0.0f && P2 != 0.0f && P1 != 0.0f ? smallest() : p;
+}
+__device__ __forceinline__ float after(float P, float S, float s) { return P == 0.0f ? S : __builtin_fmaf(P, s, S); }
+
+// One lane's V columns.  NI: the inner axis is the sequence (one environment per column);
+// else it is the channel, rows of several sequences in one where they lie end to end.
+template <int V, bool NI> struct Columns {
+  bool active;
+  int o, ib, shift;    // row, first column loaded, columns of it that belong to the neighbour
+  int na, kb;          // NI false: sequence of column ib; columns k >= kb belong to the next one
+
+  __device__ __forceinline__ Columns(const ScanArgs& a, int tile, int lane) {
+    const int64_t id = (int64_t)tile * 64 + lane, all = (int64_t)a.Lo * a.nvec;
+    active = id < all;
+    const int64_t q = active ? id : all - 1;
+    o = (int)(q / a.nvec);
+    const int i0 = (int)(q - (int64_t)o * a.nvec) * V;
+    ib = min(i0, a.Li - V);
+    shift = i0 - ib;
+    if (NI) {
+      na = ib;
+      kb = V;
+    } else {
+      na = o + ib / a.c;
+      kb = a.c - ib % a.c;
+    }
+  }
+  __device__ __forceinline__ int seq(int k) const { return NI ? ib + k : na + (k >= kb); }
+  __device__ __forceinline__ int64_t state_at(const ScanArgs& a, const SeqState& s, int k) const {
+    const int ch = NI ? o : ib % a.c + k - (k >= kb ? a.c : 0);
+    return seq(k) * s.sn + ch * s.sc;
+  }
+  __device__ __forceinline__ int64_t at(const SeqTensor& t) const { return o * t.so + ib * t.si; }
+  template <class T> __device__ __forceinline__ T* base(const SeqTensor& t) const {
+    return reinterpret_cast<T*>(t.p) + at(t);
+  }
+
+  // Bits of the columns whose episode ended at a step, of those whose sequence is over by it.
+  // Flags and lengths are loaded apart from their use (Flags below).
+  static constexpr int NF = NI ? V : (V > 1 ? 2 : 1);
+  struct Flags { float f[NF]; };
+  __device__ __forceinline__ Flags load_done(const ScanArgs& a, int t) const {
+    Flags r;
+    const float* p = a.done + (int64_t)t * a.n;
+    if constexpr (NI) {
+#pragma unroll
+      for (int k = 0; k < V; ++k) r.f[k] = p[ib + k];
+    } else {
+      r.f[0] = p[na];
+      if constexpr (V > 1) r.f[1] = p[min(na + 1, a.n - 1)];
+    }
+    return r;
+  }
+  __device__ __forceinline__ uint32_t bits(const bool* b) const {
+    if constexpr (NI) {
+      uint32_t m = 0;
+#pragma unroll
+      for (int k = 0; k < V; ++k) m |= (uint32_t)b[k] << k;
+      return m;
+    } else if constexpr (V == 1) {
+      return b[0];
+    } else {
+      const uint32_t lo = kb >= V ? (1u << V) - 1u : (1u << kb) - 1u;
+      return (b[0] ? lo : 0u) | (b[1] ? ((1u << V) - 1u) & ~lo : 0u);
+    }
+  }
+  __device__ __forceinline__ uint32_t ended(const Flags& d) const {
+    bool b[NF];
+#pragma unroll
+    for (int k = 0; k < NF; ++k) b[k] = d.f[k] != 0.0f;
+    return bits(b);
+  }
+  struct Lens { int v[NF]; };
+  __device__ __forceinline__ Lens load_lens(const ScanArgs& a) const {
+    Lens r;
+#pragma unroll
+    for (int k = 0; k < NF; ++k) r.v[k] = a.lens ? a.lens[NI ? ib + k : min(na + k, a.n - 1)] : a.T;
+    return r;
+  }
+  __device__ __forceinline__ uint32_t over(const Lens& l, int t) const {
+    bool b[NF];
+#pragma unroll
+    for (int k = 0; k < NF; ++k) b[k] = t >= l.v[k];
+    return bits(b);
+  }
+};
+
+template <class T, int V>
+__device__ __forceinline__ void load_vec(Vec<T, V>& r, const T* p, int64_t off) { r.load(p + off); }
+
+// (P, S) of V columns in LDS or in the workspace: [V][2][64], a lane's values 64 floats apart
+template <int V> __device__ __forceinline__ void put_range(float* p, int lane, const float* P, const float* S) {
+#pragma unroll
+  for (int k = 0; k < V; ++k) {
+    p[(2 * k) * 64 + lane] = P[k];
+    p[(2 * k + 1) * 64 + lane] = S[k];
+  }
+}
+template <int V> __device__ __forceinline__ void run_range(const float* p, int lane, float* s) {
+#pragma unroll
+  for (int k = 0; k < V; ++k) s[k] = after(p[(2 * k) * 64 + lane], p[(2 * k + 1) * 64 + lane], s[k]);
+}
+template <int V> __device__ __forceinline__ void join_range(const float* p, int lane, float* P, float* S) {
+#pragma unroll
+  for (int k = 0; k < V; ++k) {
+    const float p2 = p[(2 * k) * 64 + lane], s2 = p[(2 * k + 1) * 64 + lane];
+    S[k] = after(p2, s2, S[k]);
+    P[k] = chain(p2, P[k]);
+  }
+}
+// The P of a wave's own steps: zero where a cut lies in them, never by underflow
+template <int V> __device__ __forceinline__ void mark_cut(float* P, uint32_t cut) {
+#pragma unroll
+  for (int k = 0; k < V; ++k) P[k] = cut >> k & 1u ? 0.0f : (P[k] == 0.0f ? smallest() : P[k]);
+}
+
+// Steps per wave and round: as many as keep a vector's gate and input within 32 registers each
+template <int V> constexpr int scan_steps() { return V == 8 ? 4 : 8; }
+
+// launches implemented in scan.hip (shape and argument checks) and scan_backward.hip
+struct ScanShape {
+  int V, W, K;
+  bool ni;
+};
+int launch_scan_forward(const ScanArgs& a, const ScanShape& sh, bool bf16, bool sig, hipStream_t s);
+int launch_scan_backward(const ScanArgs& a, const ScanShape& sh, bool bf16, bool sig, hipStream_t s);
+
+// The instance of kernel family KERN for a shape: KERN<T, V, SIG, MASK, NI>
+#define AUV_SCAN_PICK(KERN, T, V, SIG)                                                            \
+  (mask ? (sh.ni ? (const void*)KERN<T, V, SIG, true, true> : (const void*)KERN<T, V, SIG, true, false>) \
+        : (const void*)KERN<T, V, SIG, false, false>)
+#define AUV_SCAN_KERNEL(KERN)                                                                     \
+  (bf16 ? (sh.V == 8   ? (sig ? AUV_SCAN_PICK(KERN, __bf16, 8, true) : AUV_SCAN_PICK(KERN, __bf16, 8, false)) \
+           : sh.V == 2 ? (sig ? AUV_SCAN_PICK(KERN, __bf16, 2, true) : AUV_SCAN_PICK(KERN, __bf16, 2, false)) \
+                       : (sig ? AUV_SCAN_PICK(KERN, __bf16, 1, true) : AUV_SCAN_PICK(KERN, __bf16, 1, false))) \
+        : (sh.V == 4 ? (sig ? AUV_SCAN_PICK(KERN, float, 4, true) : AUV_SCAN_PICK(KERN, float, 4, false))    \
+                     : (sig ? AUV_SCAN_PICK(KERN, float, 1, true) : AUV_SCAN_PICK(KERN, float, 1, false))))
+
+}  // namespace auv

@@ -1,0 +1,240 @@
+// Gated linear recurrence, gradient (scan.hip: the forward pass, shapes and argument checks).
+// With G_t the gradient that reaches the state after step t (G_{T-1} = dlast):
+//   g_t = dh_t + (1 - done_t) G_t,  G_{t-1} = f_t g_t,  dh0 = G_{-1}
+//   sigmoid: dx = (1 - f) g, dgate = f (1 - f) (s_{t-1} - x) g;  decay: dx = g, dgate = s_{t-1} g
+//   held steps: dx = dgate = 0, G_{t-1} = dh_t + G_t.
+// The same ranges as forward, run from the last step to the first: G before a range is P G + S of
+// the G after it.
+#include "scan.hpp"
+
+namespace auv {
+
+template <class T, int V, int U, bool SIG, bool MASK, bool NI>
+struct BackwardSteps {
+  Vec<T, V> z[U], dh[U];
+  typename Columns<V, NI>::Flags d[MASK ? U : 1];
+
+  __device__ __forceinline__ void load(const ScanArgs& a, const Columns<V, NI>& col, const T* gate, const T* dout, int t0,
+                                       int tend) {
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      if (t0 + u < tend) {
+        z[u].load(gate + (int64_t)(t0 + u) * a.gate.st);
+        if (a.dout.p) dh[u].load(dout + (int64_t)(t0 + u) * a.dout.st);
+        else dh[u].w = 0;
+        if constexpr (MASK)
+          if (a.done) d[u] = col.load_done(a, t0 + u);
+      }
+    }
+  }
+  __device__ __forceinline__ void masks(const ScanArgs& a, const Columns<V, NI>& col,
+                                        const typename Columns<V, NI>::Lens& len, int u, int t, uint32_t& done,
+                                        uint32_t& hold) const {
+    hold = col.over(len, t);
+    done = a.done ? col.ended(d[u]) & ~hold : 0u;
+  }
+  // f and the weight 1 - f of the input
+  __device__ __forceinline__ void gates(int u, int k, uint32_t hold, float& f, float& in) const {
+    if constexpr (SIG) {
+      sigmoid2<T>(z[u].get(k), f, in);
+    } else {
+      f = z[u].get(k);
+      in = 1.0f;
+    }
+    if (MASK && (hold >> k & 1u)) {
+      f = 1.0f;
+      in = 0.0f;
+    }
+  }
+};
+
+// (P, S) of every chunk of steps but the first
+template <class T, int V, bool SIG, bool MASK, bool NI>
+__global__ __launch_bounds__(1024) void k_scan_grad_ranges(ScanArgs a) {
+  constexpr int U = scan_steps<V>();
+  extern __shared__ float lds[];   // [W][V][2][64]
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), W = blockDim.x >> 6;
+  const Columns<V, NI> col(a, blockIdx.x, lane);
+  const T* gate = col.template base<T>(a.gate);
+  const T* dout = a.dout.p ? col.template base<T>(a.dout) : nullptr;
+  typename Columns<V, NI>::Lens len{};
+  if constexpr (MASK) len = col.load_lens(a);
+  const int chunk = blockIdx.y + 1;
+  const int part = a.chunk / W, tb = chunk * a.chunk + wave * part, te = min(a.T, tb + part);
+  float P[V], S[V];
+#pragma unroll
+  for (int k = 0; k < V; ++k) P[k] = 1.0f, S[k] = 0.0f;
+  uint32_t cut = 0;
+  for (int t0 = tb + part - U; t0 >= tb; t0 -= U) {
+    BackwardSteps<T, V, U, SIG, MASK, NI> st;
+    st.load(a, col, gate, dout, t0, te);
+#pragma unroll
+    for (int u = U - 1; u >= 0; --u) {
+      if (t0 + u < te) {
+        uint32_t done = 0, hold = 0;
+        if constexpr (MASK) st.masks(a, col, len, u, t0 + u, done, hold);
+#pragma unroll
+        for (int k = 0; k < V; ++k) {
+          float f, in;
+          st.gates(u, k, hold, f, in);
+          if (MASK && (done >> k & 1u)) P[k] = 1.0f, S[k] = 0.0f;
+          P[k] *= f;
+          S[k] = f * (st.dh[u].get(k) + S[k]);
+        }
+        cut |= done;
+      }
+    }
+  }
+  mark_cut<V>(P, cut);
+  put_range<V>(lds + wave * 128 * V, lane, P, S);
+  __syncthreads();
+  if (wave != W - 1) return;
+  for (int w = W - 2; w >= 0; --w) join_range<V>(lds + w * 128 * V, lane, P, S);
+  put_range<V>(a.agg + ((int64_t)chunk * a.tiles + blockIdx.x) * 128 * V, lane, P, S);
+}
+
+template <class T, int V, bool SIG, bool MASK, bool NI>
+__global__ __launch_bounds__(1024) void k_scan_backward(ScanArgs a) {
+  constexpr int U = scan_steps<V>();
+  extern __shared__ float lds[];   // [2][W][V][2][64], by round parity
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), W = blockDim.x >> 6;
+  const Columns<V, NI> col(a, blockIdx.x, lane);
+  const T *gate = col.template base<T>(a.gate), *in = col.template base<T>(a.x), *hp = col.template base<T>(a.h);
+  const T* dout = a.dout.p ? col.template base<T>(a.dout) : nullptr;
+  T *dgate = col.template base<T>(a.dgate), *dx = col.template base<T>(a.dx);
+  typename Columns<V, NI>::Lens len{};
+  if constexpr (MASK) len = col.load_lens(a);
+  const int tb = blockIdx.y * a.chunk, te = min(a.T, tb + a.chunk);
+
+  float G[V];
+#pragma unroll
+  for (int k = 0; k < V; ++k) G[k] = a.last.p ? a.last.p[col.state_at(a, a.last, k)] : 0.0f;
+  const int later = a.K - 1 - (int)blockIdx.y;
+  if (later) {   // the chunks after this one, a part per wave
+    float P[V], S[V];
+#pragma unroll
+    for (int k = 0; k < V; ++k) P[k] = 1.0f, S[k] = 0.0f;
+    const int j0 = (int)((int64_t)wave * later / W), j1 = (int)((int64_t)(wave + 1) * later / W);
+    for (int j = j0; j < j1; ++j)   // from the last chunk down
+      join_range<V>(a.agg + ((int64_t)(a.K - 1 - j) * a.tiles + blockIdx.x) * 128 * V, lane, P, S);
+    put_range<V>(lds + (W + wave) * 128 * V, lane, P, S);
+    __syncthreads();
+    for (int w = 0; w < W; ++w) run_range<V>(lds + (W + w) * 128 * V, lane, G);
+  }
+
+  int parity = 0;
+  const int span = W * U;
+  for (int r0 = tb + (te - tb - 1) / span * span; r0 >= tb; r0 -= span, parity ^= 1) {
+    const int t0 = r0 + wave * U;
+    BackwardSteps<T, V, U, SIG, MASK, NI> st;
+    st.load(a, col, gate, dout, t0, te);
+    Vec<T, V> x[U], hb[U];      // the input, the output of the step before
+    typename Columns<V, NI>::Flags db{};   // done of the step before t0
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      if (t0 + u < te) {
+        if constexpr (SIG) x[u].load(in + (int64_t)(t0 + u) * a.x.st);
+        if (t0 + u > 0) hb[u].load(hp + (int64_t)(t0 + u - 1) * a.h.st);
+      }
+    }
+    if constexpr (MASK)
+      if (a.done && t0 > 0 && t0 < te) db = col.load_done(a, t0 - 1);
+    float f[U][V], w1[U][V];
+    uint32_t done[U], hold[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      done[u] = hold[u] = 0;
+      if (t0 + u < te) {
+        if constexpr (MASK) st.masks(a, col, len, u, t0 + u, done[u], hold[u]);
+#pragma unroll
+        for (int k = 0; k < V; ++k) st.gates(u, k, hold[u], f[u][k], w1[u][k]);
+      } else {
+#pragma unroll
+        for (int k = 0; k < V; ++k) f[u][k] = 1.0f, w1[u][k] = 0.0f;
+        st.dh[u].w = 0;
+      }
+    }
+    float before[V];   // G before the round's first step
+    if (W > 1) {
+      float P[V], S[V];
+      uint32_t cut = 0;
+#pragma unroll
+      for (int k = 0; k < V; ++k) P[k] = 1.0f, S[k] = 0.0f;
+#pragma unroll
+      for (int u = U - 1; u >= 0; --u) {
+#pragma unroll
+        for (int k = 0; k < V; ++k) {
+          if (MASK && (done[u] >> k & 1u)) P[k] = 1.0f, S[k] = 0.0f;
+          P[k] *= f[u][k];
+          S[k] = f[u][k] * (st.dh[u].get(k) + S[k]);
+        }
+        cut |= done[u];
+      }
+      mark_cut<V>(P, cut);
+      float* x_ = lds + parity * W * 128 * V;
+      put_range<V>(x_ + wave * 128 * V, lane, P, S);
+      __syncthreads();
+      for (int w = W - 1; w > wave; --w) run_range<V>(x_ + w * 128 * V, lane, G);
+#pragma unroll
+      for (int k = 0; k < V; ++k) before[k] = G[k];
+      for (int w = wave; w >= 0; --w) run_range<V>(x_ + w * 128 * V, lane, before);
+    }
+#pragma unroll
+    for (int u = U - 1; u >= 0; --u) {
+      if (t0 + u < te) {
+        const int t = t0 + u;
+        uint32_t fresh = 0;   // columns whose state before this step is a new episode's zero
+        if constexpr (MASK) {
+          if (u) fresh = done[u > 0 ? u - 1 : 0];
+          else if (a.done && t > 0) fresh = col.ended(db);
+        }
+        float gz[V], gx[V];
+#pragma unroll
+        for (int k = 0; k < V; ++k) {
+          if (MASK && (done[u] >> k & 1u)) G[k] = 0.0f;
+          const float g = st.dh[u].get(k) + G[k];
+          float sp;
+          if (t > 0) sp = MASK && (fresh >> k & 1u) ? 0.0f : hb[u].get(k);
+          else sp = a.h0.p ? a.h0.p[col.state_at(a, a.h0, k)] : 0.0f;
+          if constexpr (SIG) {
+            gx[k] = w1[u][k] * g;
+            gz[k] = f[u][k] * (sp - x[u].get(k)) * gx[k];
+          } else {
+            gx[k] = g;
+            gz[k] = sp * g;
+          }
+          if (MASK && (hold[u] >> k & 1u)) gx[k] = gz[k] = 0.0f;
+          G[k] = f[u][k] * g;
+        }
+        if (col.active) {
+          store_own<T, V>(dgate + (int64_t)t * a.dgate.st, gz, col.shift);
+          store_own<T, V>(dx + (int64_t)t * a.dx.st, gx, col.shift);
+        }
+      }
+    }
+    if (W > 1) {
+#pragma unroll
+      for (int k = 0; k < V; ++k) G[k] = before[k];
+    }
+  }
+  if (a.dh0.p && blockIdx.y == 0 && wave == 0 && col.active) {
+#pragma unroll
+    for (int k = 0; k < V; ++k)
+      if (k >= col.shift) a.dh0.p[col.state_at(a, a.dh0, k)] = G[k];
+  }
+}
+
+int launch_scan_backward(const ScanArgs& a, const ScanShape& sh, bool bf16, bool sig, hipStream_t s) {
+  const bool mask = a.done || a.lens;
+  ScanArgs arg = a;
+  void* args[1] = {&arg};
+  const size_t range = sizeof(float) * 128 * sh.V;
+  if (sh.K > 1)
+    if (int rc = launch_kernel("auv_scan_backward", AUV_SCAN_KERNEL(k_scan_grad_ranges), dim3(a.tiles, sh.K - 1),
+                               dim3(64 * sh.W), args, sh.W * range, s))
+      return rc;
+  return launch_kernel("auv_scan_backward", AUV_SCAN_KERNEL(k_scan_backward), dim3(a.tiles, sh.K), dim3(64 * sh.W), args,
+                       2 * sh.W * range, s);
+}
+
+}  // namespace auv

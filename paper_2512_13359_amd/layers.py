@@ -1,0 +1,232 @@
+"""Network layers over rollouts as functions of torch tensors on the GPU: the gated linear
+recurrence, group norm with an activation, dropout from the counter-based generator, each with its
+gradient (auv_scan_*, auv_norm_*, auv_dropout).  Argument checks, allocation and marshalling only.
+
+Outputs and workspaces are torch allocations made on the stream that the call runs on: the current
+stream of the tensors' device, or `stream`.  Nothing is kept between calls, so calls may be captured
+into a graph.  The functions are not part of torch's autograd: gradients come from the *_backward
+functions.  Wrong arguments raise AuvError before anything is enqueued."""
+from __future__ import annotations
+
+import torch
+
+from . import _abi as A
+
+TYPES = {torch.float32: A.AUV_FP32, torch.bfloat16: A.AUV_BF16}
+KINDS = {"sigmoid": A.AUV_SCAN_SIGMOID, "decay": A.AUV_SCAN_DECAY}
+ACTS = {"none": A.AUV_ACTIVATION_NONE, "relu": A.AUV_ACTIVATION_RELU, "silu": A.AUV_ACTIVATION_SILU,
+        "tanh": A.AUV_ACTIVATION_TANH}
+
+
+def _refuse(fn: str, msg: str):
+    raise A.AuvError(A.AUV_EINVAL, f"{fn}: {msg}")
+
+
+def _one_of(fn, what, choices, v):
+    if v not in choices:
+        _refuse(fn, f"{what} must be one of {', '.join(map(str, choices))}, got {v}")
+    return choices[v]
+
+
+def _like(fn, name, t, shape, dtype, device, contiguous=False):
+    """Checks an optional tensor; returns it."""
+    if t is None:
+        return None
+    if t.dtype != dtype or tuple(t.shape) != shape:
+        _refuse(fn, f"{name} must be {dtype} of shape {tuple(shape)}, got {t.dtype} of {tuple(t.shape)}")
+    if t.device != device:
+        _refuse(fn, f"{name} is on {t.device}, x on {device}")
+    if contiguous and not t.is_contiguous():
+        _refuse(fn, f"{name} must be contiguous")
+    return t
+
+
+def _here(fn, x, stream) -> bool:
+    """Whether x's device is the current one and the stream its current stream."""
+    if not x.is_cuda:
+        _refuse(fn, f"tensors must be on a GPU, x is on {x.device}")
+    return stream is None and x.device.index == torch.cuda.current_device()
+
+
+def _moved(x, stream):
+    """Makes x's device and the stream current: the call inside allocates and launches there."""
+    class Scope:
+        def __enter__(self):
+            self.d = torch.cuda.device(x.device)
+            self.d.__enter__()
+            self.s = torch.cuda.stream(stream)
+            self.s.__enter__()
+
+        def __exit__(self, *e):
+            self.s.__exit__(*e)
+            self.d.__exit__(*e)
+    return Scope()
+
+
+def _empty(n: int, x) -> torch.Tensor | None:
+    return torch.empty(n, dtype=torch.uint8, device=x.device) if n else None
+
+
+# ---- gated linear recurrence ---------------------------------------------------------
+
+def _scan(fn, gate, x, kind, done, lens, h0):
+    if x.dim() != 3 or x.dtype not in TYPES:
+        _refuse(fn, f"x must be a float32 or bfloat16 tensor [T][n][c], got {x.dtype} of {tuple(x.shape)}")
+    T, n, c = x.shape
+    dev = x.device
+    _like(fn, "gate", gate, x.shape, x.dtype, dev)
+    _like(fn, "done", done, (T, n), torch.float32, dev, True)
+    _like(fn, "lens", lens, (n,), torch.int32, dev, True)
+    _like(fn, "h0", h0, (n, c), torch.float32, dev)
+    return T, n, c
+
+
+def _seq(t):
+    return (0, 0, 0, 0) if t is None else (t.data_ptr(), *t.stride())
+
+
+def _state(t):
+    return (0, 0, 0) if t is None else (t.data_ptr(), *t.stride())
+
+
+def scan_forward(gate, x, *, kind="sigmoid", done=None, lens=None, h0=None, out=None, stream=None):
+    """Gated linear recurrence over the steps of a rollout; returns (h, last).
+
+    gate, x: [T][n][c], float32 or bfloat16, in any memory order.  With s_{-1} = h0 (zero if None):
+      kind "sigmoid": f = sigma(gate), h_t = f s_{t-1} + (1 - f) x_t
+      kind "decay":   f = gate,        h_t = f s_{t-1} + x_t
+    and s_t = 0 where done [T][n] (float32, contiguous, as a rollout records it) is nonzero, else h_t.
+    lens [n] (int32): from a sequence's length on the state is held, h_t = s_t = s_{t-1}.
+    h has x's type and memory order, or is `out`; last = s_{T-1} and h0 are float32 [n][c].  One step
+    (T = 1) is the form for a controller: pass `last` back as the next h0."""
+    fn = "scan_forward"
+    T, n, c = _scan(fn, gate, x, kind, done, lens, h0)
+    k = _one_of(fn, "kind", KINDS, kind)
+    _like(fn, "out", out, x.shape, x.dtype, x.device)
+    if not _here(fn, x, stream):
+        with _moved(x, stream):
+            return scan_forward(gate, x, kind=kind, done=done, lens=lens, h0=h0, out=out)
+    h = torch.empty_like(x) if out is None else out
+    last = torch.empty((n, c), dtype=torch.float32, device=x.device) if h0 is None else torch.empty_like(h0)
+    d = A.AuvScan(T, n, c, TYPES[x.dtype], k, *_seq(gate), *_seq(x), *_seq(h), A.ptr(done), A.ptr(lens), *_state(h0),
+                  *_state(last))
+    A.auv_scan_forward(d, _empty(A.auv_scan_work_bytes(d), x))
+    return h, last
+
+
+def scan_backward(gate, x, h, *, dout=None, dh_last=None, kind="sigmoid", done=None, lens=None, h0=None, out=None,
+                  stream=None):
+    """Gradients (dgate, dx, dh0) of scan_forward from those of its results, dout (of h) and dh_last
+    (of last); None stands for zero.  h is scan_forward's result, the other arguments its own.
+    dgate and dx have x's type (zero at held steps), or are the pair `out`: the halves of one
+    buffer, say, where gate and x are the halves of one projection.  dh0 is float32 [n][c]."""
+    fn = "scan_backward"
+    T, n, c = _scan(fn, gate, x, kind, done, lens, h0)
+    k = _one_of(fn, "kind", KINDS, kind)
+    _like(fn, "h", h, x.shape, x.dtype, x.device)
+    _like(fn, "dout", dout, x.shape, x.dtype, x.device)
+    _like(fn, "dh_last", dh_last, (n, c), torch.float32, x.device)
+    for o in out or ():
+        _like(fn, "out", o, x.shape, x.dtype, x.device)
+    if not _here(fn, x, stream):
+        with _moved(x, stream):
+            return scan_backward(gate, x, h, dout=dout, dh_last=dh_last, kind=kind, done=done, lens=lens, h0=h0, out=out)
+    dgate, dx = (torch.empty_like(gate), torch.empty_like(x)) if out is None else out
+    like = h0 if h0 is not None else dh_last
+    dh0 = torch.empty((n, c), dtype=torch.float32, device=x.device) if like is None else torch.empty_like(like)
+    d = A.AuvScan(T, n, c, TYPES[x.dtype], k, *_seq(gate), *_seq(x), *_seq(h), A.ptr(done), A.ptr(lens), *_state(h0))
+    g = A.AuvScanGrad(*_seq(dout), *_state(dh_last), *_seq(dgate), *_seq(dx), *_state(dh0))
+    A.auv_scan_backward(d, g, _empty(A.auv_scan_work_bytes(d, g), x))
+    return dgate, dx, dh0
+
+
+# ---- group norm and dropout ----------------------------------------------------------
+
+def _rows(fn, name, t):
+    """(n, s, c) of a channels-last tensor [n][c] or [n][s][c]."""
+    if t.dim() not in (2, 3) or t.dtype not in TYPES:
+        _refuse(fn, f"{name} must be a float32 or bfloat16 tensor [n][c] or [n][s][c], got {t.dtype} of {tuple(t.shape)}")
+    return (t.shape[0], 1, t.shape[1]) if t.dim() == 2 else tuple(t.shape)
+
+
+def _at(fn, name, t):
+    """Address and strides (sample, position) of a channels-last tensor."""
+    st = t.stride()
+    if st[-1] != 1 and t.shape[-1] != 1:
+        _refuse(fn, f"{name} must have its channels last with stride 1, got strides {st}")
+    return (t.data_ptr(), st[0], 0 if len(st) == 2 else st[1])
+
+
+def _fresh(x):
+    """A new tensor of x's shape and type whose channels have stride 1."""
+    return torch.empty(x.shape, dtype=x.dtype, device=x.device)
+
+
+def dropout(x, drop, add=None, *, out=None, stream=None):
+    """Dropout of x, [n][c] or [n][s][c] with channels last, by the draws of `drop` (make_drop), plus `add` where given.
+    No mask is stored: the gradient is dropout of the gradient with the same `drop`.  `out` may be x or
+    add itself."""
+    fn = "dropout"
+    n, s, c = _rows(fn, "x", x)
+    _like(fn, "add", add, x.shape, x.dtype, x.device)
+    _like(fn, "out", out, x.shape, x.dtype, x.device)
+    if not _here(fn, x, stream):
+        with _moved(x, stream):
+            return dropout(x, drop, add, out=out)
+    y = _fresh(x) if out is None else out
+    A.auv_dropout(drop, TYPES[x.dtype], n, s, c, A.AuvRows(*_at(fn, "x", x)),
+                  None if add is None else A.AuvRows(*_at(fn, "add", add)), A.AuvRows(*_at(fn, "out", y)))
+    return y
+
+
+def _norm(fn, x, groups, weight, bias, eps, act, drop, mean, rstd):
+    n, s, c = _rows(fn, "x", x)
+    _like(fn, "weight", weight, (c,), torch.float32, x.device, True)
+    _like(fn, "bias", bias, (c,), torch.float32, x.device, True)
+    # the callers hold `drop` while the structure is in use
+    return A.AuvNorm(n, s, c, groups, TYPES[x.dtype], _one_of(fn, "act", ACTS, act), eps, *_at(fn, "x", x), A.ptr(weight),
+                     A.ptr(bias), A.ptr(mean), A.ptr(rstd), None if drop is None else A.address(drop))
+
+
+def norm_forward(x, groups, *, weight=None, bias=None, eps=1e-5, act="none", drop=None, out=None, stream=None):
+    """Group norm with an activation; returns (y, mean, rstd).
+
+    x: [n][c] or [n][s][c], float32 or bfloat16, channels last.  Mean and variance are taken over the s
+    positions and c / groups channels of each group of each sample (groups = 1 and no positions: layer
+    norm); y = act(weight xhat + bias), weight and bias float32 [c] or None, act one of "none", "relu",
+    "silu", "tanh".  With `drop` (make_drop) x is dropped out first, its mask never stored.  mean and
+    rstd are float32 [n][groups]; y has x's type, or is `out`."""
+    fn = "norm_forward"
+    d = _norm(fn, x, groups, weight, bias, eps, act, drop, None, None)
+    _like(fn, "out", out, x.shape, x.dtype, x.device)
+    if not _here(fn, x, stream):
+        with _moved(x, stream):
+            return norm_forward(x, groups, weight=weight, bias=bias, eps=eps, act=act, drop=drop, out=out)
+    work = _empty(A.auv_norm_work_bytes(d, False), x)
+    y = _fresh(x) if out is None else out
+    mean = torch.empty((d.n, groups), dtype=torch.float32, device=x.device)
+    rstd = torch.empty_like(mean)
+    d.mean, d.rstd = mean.data_ptr(), rstd.data_ptr()
+    A.auv_norm_forward(d, A.AuvRows(*_at(fn, "out", y)), work)
+    return y, mean, rstd
+
+
+def norm_backward(x, groups, mean, rstd, dout, *, weight=None, bias=None, act="none", drop=None, out=None, stream=None):
+    """Gradients (dx, dweight, dbias) of norm_forward from that of y; mean and rstd are its results, the
+    other arguments its own.  dx has x's type, or is `out`; dweight is None where weight is, dbias
+    where bias is, else float32 [c]."""
+    fn = "norm_backward"
+    d = _norm(fn, x, groups, weight, bias, 0.0, act, drop, mean, rstd)
+    for name, t in (("mean", mean), ("rstd", rstd)):
+        _like(fn, name, t, (d.n, groups), torch.float32, x.device, True)
+    _like(fn, "dout", dout, x.shape, x.dtype, x.device)
+    _like(fn, "out", out, x.shape, x.dtype, x.device)
+    if not _here(fn, x, stream):
+        with _moved(x, stream):
+            return norm_backward(x, groups, mean, rstd, dout, weight=weight, bias=bias, act=act, drop=drop, out=out)
+    work = _empty(A.auv_norm_work_bytes(d, True), x)
+    dx = _fresh(x) if out is None else out
+    dweight = None if weight is None else torch.empty_like(weight)
+    dbias = None if bias is None else torch.empty_like(bias)
+    A.auv_norm_backward(d, A.AuvNormGrad(*_at(fn, "dout", dout), *_at(fn, "out", dx), A.ptr(dweight), A.ptr(dbias)), work)
+    return dx, dweight, dbias
