@@ -14,6 +14,7 @@ namespace auv {
 template <int BYTES> struct WordOf;
 template <> struct WordOf<2> { typedef uint16_t type __attribute__((may_alias)); };
 template <> struct WordOf<4> { typedef uint32_t type __attribute__((aligned(2), may_alias)); };
+template <> struct WordOf<8> { typedef uint32_t type __attribute__((ext_vector_type(2), aligned(2), may_alias)); };
 template <> struct WordOf<16> { typedef uint32_t type __attribute__((ext_vector_type(4), aligned(2), may_alias)); };
 
 template <class T, int V> struct Vec {

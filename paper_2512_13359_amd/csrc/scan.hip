@@ -17,11 +17,12 @@ struct ForwardSteps {
 
   __device__ __forceinline__ void load(const ScanArgs& a, const Columns<V, NI>& col, const T* gate, const T* in, int t0,
                                        int tend) {
+    const T *pz = gate + t0 * a.gate.st, *px = in + t0 * a.x.st;
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
+    for (int u = 0; u < U; ++u, pz += a.gate.st, px += a.x.st) {
       if (t0 + u < tend) {
-        z[u].load(gate + (int64_t)(t0 + u) * a.gate.st);
-        x[u].load(in + (int64_t)(t0 + u) * a.x.st);
+        z[u].load(pz);
+        x[u].load(px);
         if constexpr (MASK)
           if (a.done) d[u] = col.load_done(a, t0 + u);
       }
@@ -33,27 +34,47 @@ struct ForwardSteps {
     hold = col.over(len, t);
     done = a.done ? col.ended(d[u]) & ~hold : 0u;
   }
-  __device__ __forceinline__ void step(int u, int k, uint32_t hold, float& f, float& in) const {
-    const float zz = z[u].get(k), xx = x[u].get(k);
-    if constexpr (SIG) {
-      float g;
-      sigmoid2<T>(zz, f, g);
-      in = g * xx;
-    } else {
-      f = zz;
-      in = xx;
+  // f and the input's share of one step
+  __device__ __forceinline__ void step(int u, uint32_t hold, float* f, float* in) const {
+#pragma unroll
+    for (int k = 0; k < V; ++k) {
+      const float zz = z[u].get(k), xx = x[u].get(k);
+      if constexpr (SIG) {
+        float g;
+        sigmoid2<T>(zz, f[k], g);
+        in[k] = g * xx;
+      } else {
+        f[k] = zz;
+        in[k] = xx;
+      }
     }
-    if (MASK && (hold >> k & 1u)) {
-      f = 1.0f;
-      in = 0.0f;
+    if (MASK && any_lane(hold)) {
+#pragma unroll
+      for (int k = 0; k < V; ++k)
+        if (hold >> k & 1u) f[k] = 1.0f, in[k] = 0.0f;
     }
   }
 };
 
+// One more step of a range's (P, S)
+template <bool MASK, int V>
+__device__ __forceinline__ void append(float* P, float* S, const float* f, const float* in, uint32_t done) {
+#pragma unroll
+  for (int k = 0; k < V; ++k) {
+    P[k] *= f[k];
+    S[k] = __builtin_fmaf(f[k], S[k], in[k]);
+  }
+  if (MASK && any_lane(done)) {
+#pragma unroll
+    for (int k = 0; k < V; ++k)
+      if (done >> k & 1u) P[k] = 1.0f, S[k] = 0.0f;
+  }
+}
+
 // (P, S) of every chunk of steps but the last: each wave runs a contiguous part of its chunk, the
 // first wave joins the parts.
 template <class T, int V, bool SIG, bool MASK, bool NI>
-__global__ __launch_bounds__(1024) void k_scan_ranges(ScanArgs a) {
+__global__ __launch_bounds__(64 * SCAN_WAVES) void k_scan_ranges(ScanArgs a) {
   constexpr int U = scan_steps<V>();
   extern __shared__ float lds[];   // [W][V][2][64]
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), W = blockDim.x >> 6;
@@ -74,14 +95,9 @@ __global__ __launch_bounds__(1024) void k_scan_ranges(ScanArgs a) {
       if (t0 + u < te) {
         uint32_t done = 0, hold = 0;
         if constexpr (MASK) st.masks(a, col, len, u, t0 + u, done, hold);
-#pragma unroll
-        for (int k = 0; k < V; ++k) {
-          float f, v;
-          st.step(u, k, hold, f, v);
-          P[k] *= f;
-          S[k] = __builtin_fmaf(f, S[k], v);
-          if (MASK && (done >> k & 1u)) P[k] = 1.0f, S[k] = 0.0f;
-        }
+        float f[V], v[V];
+        st.step(u, hold, f, v);
+        append<MASK, V>(P, S, f, v, done);
         cut |= done;
       }
     }
@@ -95,7 +111,7 @@ __global__ __launch_bounds__(1024) void k_scan_ranges(ScanArgs a) {
 }
 
 template <class T, int V, bool SIG, bool MASK, bool NI>
-__global__ __launch_bounds__(1024) void k_scan_forward(ScanArgs a) {
+__global__ __launch_bounds__(64 * SCAN_WAVES) void k_scan_forward(ScanArgs a) {
   constexpr int U = scan_steps<V>();
   extern __shared__ float lds[];   // [2][W][V][2][64], by round parity
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), W = blockDim.x >> 6;
@@ -121,11 +137,14 @@ __global__ __launch_bounds__(1024) void k_scan_forward(ScanArgs a) {
     for (int w = 0; w < W; ++w) run_range<V>(lds + (W + w) * 128 * V, lane, s);
   }
 
+  // the next round's loads are in flight while a round is computed
+  ForwardSteps<T, V, U, SIG, MASK, NI> next;
+  next.load(a, col, gate, in, tb + wave * U, te);
   int parity = 0;
   for (int r0 = tb; r0 < te; r0 += W * U, parity ^= 1) {
     const int t0 = r0 + wave * U;
-    ForwardSteps<T, V, U, SIG, MASK, NI> st;
-    st.load(a, col, gate, in, t0, te);
+    const ForwardSteps<T, V, U, SIG, MASK, NI> st = next;
+    next.load(a, col, gate, in, t0 + W * U, te);
     float f[U][V], v[U][V];
     uint32_t done[U];
 #pragma unroll
@@ -134,8 +153,7 @@ __global__ __launch_bounds__(1024) void k_scan_forward(ScanArgs a) {
       if (t0 + u < te) {
         uint32_t hold = 0;
         if constexpr (MASK) st.masks(a, col, len, u, t0 + u, done[u], hold);
-#pragma unroll
-        for (int k = 0; k < V; ++k) st.step(u, k, hold, f[u][k], v[u][k]);
+        st.step(u, hold, f[u], v[u]);
       } else {
 #pragma unroll
         for (int k = 0; k < V; ++k) f[u][k] = 1.0f, v[u][k] = 0.0f;
@@ -149,12 +167,7 @@ __global__ __launch_bounds__(1024) void k_scan_forward(ScanArgs a) {
       for (int k = 0; k < V; ++k) P[k] = 1.0f, S[k] = 0.0f;
 #pragma unroll
       for (int u = 0; u < U; ++u) {
-#pragma unroll
-        for (int k = 0; k < V; ++k) {
-          P[k] *= f[u][k];
-          S[k] = __builtin_fmaf(f[u][k], S[k], v[u][k]);
-          if (MASK && (done[u] >> k & 1u)) P[k] = 1.0f, S[k] = 0.0f;
-        }
+        append<MASK, V>(P, S, f[u], v[u], done[u]);
         cut |= done[u];
       }
       mark_cut<V>(P, cut);
@@ -166,16 +179,19 @@ __global__ __launch_bounds__(1024) void k_scan_forward(ScanArgs a) {
       for (int k = 0; k < V; ++k) end[k] = s[k];
       for (int w = wave; w < W; ++w) run_range<V>(x + w * 128 * V, lane, end);
     }
+    T* po = out + t0 * a.h.st;
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
+    for (int u = 0; u < U; ++u, po += a.h.st) {
       if (t0 + u < te) {
         float h[V];
 #pragma unroll
-        for (int k = 0; k < V; ++k) {
-          h[k] = __builtin_fmaf(f[u][k], s[k], v[u][k]);
-          s[k] = MASK && (done[u] >> k & 1u) ? 0.0f : h[k];
+        for (int k = 0; k < V; ++k) s[k] = h[k] = __builtin_fmaf(f[u][k], s[k], v[u][k]);
+        if (MASK && any_lane(done[u])) {
+#pragma unroll
+          for (int k = 0; k < V; ++k)
+            if (done[u] >> k & 1u) s[k] = 0.0f;
         }
-        if (col.active) store_own<T, V>(out + (int64_t)(t0 + u) * a.h.st, h, col.shift);
+        if (col.active) store_own<T, V>(po, h, col.shift);
       }
     }
     if (W > 1) {
@@ -258,7 +274,7 @@ static SeqTensor inner_first(const auv_seq& s, bool ni) {
 }
 
 // Columns, vectors, waves per workgroup and chunks for the tensors of one pass.
-static void scan_shape(const auv_scan* d, const auv_seq* const* seqs, int count, ScanArgs& a, ScanShape& sh) {
+static void scan_shape(const auv_scan* d, const auv_seq* const* seqs, int count, bool grad, ScanArgs& a, ScanShape& sh) {
   const int n = d->n, c = d->c;
   bool unit_c = true, unit_n = true, rows = true;
   for (int k = 0; k < count; ++k) {
@@ -271,22 +287,32 @@ static void scan_shape(const auv_scan* d, const auv_seq* const* seqs, int count,
   const bool unit = unit_c || unit_n, flat = !sh.ni && unit_c && rows;
   a.Li = sh.ni ? n : (flat ? n * c : c);
   a.Lo = sh.ni ? c : (flat ? 1 : n);
-  const int full = d->type == AUV_BF16 ? 8 : 4, cus = compute_units();
+  const int cus = compute_units();
   auto tiles_of = [&](int V) { return (int)(((int64_t)a.Lo * ((a.Li + V - 1) / V) + 63) / 64); };
   // A vector that straddles sequences straddles two at most.
   auto fits = [&](int V) { return unit && a.Li >= V && (sh.ni || c >= V || a.Li == c); };
-  sh.V = fits(full) ? full : 1;
-  if (sh.V == 1 && full == 8 && fits(2)) sh.V = 2;
-  if (sh.V == full && tiles_of(full) < cus / 2) sh.V = full == 8 ? 2 : 1;
+  // Wide vectors where they leave four waves per CU: bf16, 4096 x 64 columns x 512 steps, both directions: V = 4 in 495
+  // us, V = 2 535, V = 1 650, V = 8 (at its best, four waves per workgroup; more registers) 531.  Else two columns per lane: they make the
+  // fewest lane accesses that still fill the chip (37037 bf16 columns x 700: V = 4 in 204, V = 2 177, V = 1 209); but
+  // one where only that gives a workgroup per CU without splitting the steps and an access is 4 bytes all the same
+  // (fp32, 16384 columns x 1024: V = 1 in 142, V = 2 split in four 167).
+  sh.V = fits(4) && tiles_of(4) >= 4 * cus ? 4 : fits(2) && tiles_of(1) > 1 ? 2 : 1;
+  if (sh.V == 2 && d->type == AUV_FP32 && tiles_of(2) < cus && tiles_of(1) >= cus) sh.V = 1;
   a.nvec = (a.Li + sh.V - 1) / sh.V;
   a.tiles = tiles_of(sh.V);
-  const int U = sh.V == 8 ? 4 : 8, most = sh.V == 8 ? 8 : 16;   // 64 KB of LDS at most
+  const int U = sh.V >= (grad ? 2 : 4) ? 4 : 8;   // scan_steps, scan_grad_steps
+  // Waves per workgroup until there are eight per CU (4095 x 23 fp32 columns x 500 steps, 736 tiles, forward and backward: one wave
+  // 160 and 355 us, two 145 and 260, four 142 and 243; where there are eight anyway one wave is best, 16384 x 64 columns x 64 steps: 81, two
+  // waves 88).
   sh.W = 1;
-  while (sh.W < most && (int64_t)a.tiles * sh.W < 8 * cus && sh.W * U < d->T) sh.W *= 2;
+  while (sh.W < SCAN_WAVES && (int64_t)a.tiles * sh.W < 8 * cus && sh.W * U < d->T) sh.W *= 2;
   const int span = sh.W * U, rounds = (d->T - 1) / span + 1;
+  // Steps split over workgroups where there is less than one per CU, up to two per CU: reads gate and input (or dout) twice.
+  // 2048 columns x 4096 steps: whole 201 and 398 us, split in 16 30 and 43, in 32 25 and 33; 16384 columns x 1024 steps: whole 54 and
+  // 105, in four 39 and 54, in eight 46 and 59; 32768 columns (256 tiles): whole 57 and 115, in two 64 and 107.
   sh.K = 1;
   const bool in_place = d->last.p && d->last.p == d->h0.p;   // its chunks would read what the last one writes
-  if (sh.W == most && rounds >= 8 && a.tiles < cus && !in_place) sh.K = std::min((2 * cus - 1) / a.tiles + 1, rounds / 2);
+  if (sh.W == SCAN_WAVES && rounds >= 4 && a.tiles < cus && !in_place) sh.K = std::min((2 * cus - 1) / a.tiles + 1, rounds);
   a.chunk = ((rounds - 1) / sh.K + 1) * span;
   sh.K = (d->T - 1) / a.chunk + 1;
   a.K = sh.K;
@@ -299,7 +325,7 @@ static void scan_shape(const auv_scan* d, const auv_seq* const* seqs, int count,
 
 static void forward_args(const auv_scan* d, ScanArgs& a, ScanShape& sh) {
   const auv_seq* seqs[3] = {&d->gate, &d->x, &d->h};
-  scan_shape(d, seqs, 3, a, sh);
+  scan_shape(d, seqs, 3, false, a, sh);
   a.gate = inner_first(d->gate, sh.ni);
   a.x = inner_first(d->x, sh.ni);
   a.h = inner_first(d->h, sh.ni);
@@ -309,7 +335,7 @@ static void backward_args(const auv_scan* d, const auv_scan_grad* g, ScanArgs& a
   const auv_seq* seqs[6] = {&d->gate, &d->h, &g->dgate, &g->dx, &d->x, &g->dout};
   int count = 5;
   if (g->dout.p) seqs[count++] = &g->dout;
-  scan_shape(d, seqs, count, a, sh);
+  scan_shape(d, seqs, count, true, a, sh);
   a.gate = inner_first(d->gate, sh.ni);
   a.x = inner_first(d->x, sh.ni);
   a.h = inner_first(d->h, sh.ni);

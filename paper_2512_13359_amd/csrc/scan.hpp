@@ -117,23 +117,28 @@ template <int V, bool NI> struct Columns {
     for (int k = 0; k < NF; ++k) b[k] = d.f[k] != 0.0f;
     return bits(b);
   }
-  struct Lens { int v[NF]; };
+  struct Lens { int v[NF], soonest; };   // soonest: no column of the wave is over before it
   __device__ __forceinline__ Lens load_lens(const ScanArgs& a) const {
     Lens r;
+    r.soonest = a.T;
 #pragma unroll
-    for (int k = 0; k < NF; ++k) r.v[k] = a.lens ? a.lens[NI ? ib + k : min(na + k, a.n - 1)] : a.T;
+    for (int k = 0; k < NF; ++k) {
+      r.v[k] = a.lens ? a.lens[NI ? ib + k : min(na + k, a.n - 1)] : a.T;
+      r.soonest = min(r.soonest, r.v[k]);
+    }
+    if (a.lens)
+      for (int d = 1; d < 64; d <<= 1) r.soonest = min(r.soonest, __shfl_xor(r.soonest, d));
+    r.soonest = __builtin_amdgcn_readfirstlane(r.soonest);
     return r;
   }
   __device__ __forceinline__ uint32_t over(const Lens& l, int t) const {
+    if (t < l.soonest) return 0;
     bool b[NF];
 #pragma unroll
     for (int k = 0; k < NF; ++k) b[k] = t >= l.v[k];
     return bits(b);
   }
 };
-
-template <class T, int V>
-__device__ __forceinline__ void load_vec(Vec<T, V>& r, const T* p, int64_t off) { r.load(p + off); }
 
 // (P, S) of V columns in LDS or in the workspace: [V][2][64], a lane's values 64 floats apart
 template <int V> __device__ __forceinline__ void put_range(float* p, int lane, const float* P, const float* S) {
@@ -161,8 +166,13 @@ template <int V> __device__ __forceinline__ void mark_cut(float* P, uint32_t cut
   for (int k = 0; k < V; ++k) P[k] = cut >> k & 1u ? 0.0f : (P[k] == 0.0f ? smallest() : P[k]);
 }
 
-// Steps per wave and round: as many as keep a vector's gate and input within 32 registers each
-template <int V> constexpr int scan_steps() { return V == 8 ? 4 : 8; }
+// Steps per wave and round, and the most waves of a workgroup (256 registers a lane)
+template <int V> constexpr int scan_steps() { return V >= 4 ? 4 : 8; }
+template <int V> constexpr int scan_grad_steps() { return V >= 2 ? 4 : 8; }
+constexpr int SCAN_WAVES = 8;
+
+// Flags are rare: the selects for a step are jumped over where no lane of the wave has one.
+__device__ __forceinline__ bool any_lane(uint32_t bits) { return __ballot(bits != 0u) != 0ull; }
 
 // launches implemented in scan.hip (shape and argument checks) and scan_backward.hip
 struct ScanShape {
@@ -176,11 +186,13 @@ int launch_scan_backward(const ScanArgs& a, const ScanShape& sh, bool bf16, bool
 #define AUV_SCAN_PICK(KERN, T, V, SIG)                                                            \
   (mask ? (sh.ni ? (const void*)KERN<T, V, SIG, true, true> : (const void*)KERN<T, V, SIG, true, false>) \
         : (const void*)KERN<T, V, SIG, false, false>)
-#define AUV_SCAN_KERNEL(KERN)                                                                     \
-  (bf16 ? (sh.V == 8   ? (sig ? AUV_SCAN_PICK(KERN, __bf16, 8, true) : AUV_SCAN_PICK(KERN, __bf16, 8, false)) \
-           : sh.V == 2 ? (sig ? AUV_SCAN_PICK(KERN, __bf16, 2, true) : AUV_SCAN_PICK(KERN, __bf16, 2, false)) \
-                       : (sig ? AUV_SCAN_PICK(KERN, __bf16, 1, true) : AUV_SCAN_PICK(KERN, __bf16, 1, false))) \
-        : (sh.V == 4 ? (sig ? AUV_SCAN_PICK(KERN, float, 4, true) : AUV_SCAN_PICK(KERN, float, 4, false))    \
-                     : (sig ? AUV_SCAN_PICK(KERN, float, 1, true) : AUV_SCAN_PICK(KERN, float, 1, false))))
+#define AUV_SCAN_KIND(KERN, T, V) (sig ? AUV_SCAN_PICK(KERN, T, V, true) : AUV_SCAN_PICK(KERN, T, V, false))
+#define AUV_SCAN_KERNEL(KERN)                        \
+  (bf16 ? (sh.V == 4   ? AUV_SCAN_KIND(KERN, __bf16, 4) \
+           : sh.V == 2 ? AUV_SCAN_KIND(KERN, __bf16, 2) \
+                       : AUV_SCAN_KIND(KERN, __bf16, 1)) \
+        : (sh.V == 4   ? AUV_SCAN_KIND(KERN, float, 4)  \
+           : sh.V == 2 ? AUV_SCAN_KIND(KERN, float, 2)  \
+                       : AUV_SCAN_KIND(KERN, float, 1)))
 
 }  // namespace auv

@@ -16,12 +16,13 @@ struct BackwardSteps {
 
   __device__ __forceinline__ void load(const ScanArgs& a, const Columns<V, NI>& col, const T* gate, const T* dout, int t0,
                                        int tend) {
+    const T *pz = gate + t0 * a.gate.st, *pd = dout + t0 * a.dout.st;
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
+    for (int u = 0; u < U; ++u, pz += a.gate.st, pd += a.dout.st) {
+      dh[u].w = 0;
       if (t0 + u < tend) {
-        z[u].load(gate + (int64_t)(t0 + u) * a.gate.st);
-        if (a.dout.p) dh[u].load(dout + (int64_t)(t0 + u) * a.dout.st);
-        else dh[u].w = 0;
+        z[u].load(pz);
+        if (a.dout.p) dh[u].load(pd);
         if constexpr (MASK)
           if (a.done) d[u] = col.load_done(a, t0 + u);
       }
@@ -34,24 +35,41 @@ struct BackwardSteps {
     done = a.done ? col.ended(d[u]) & ~hold : 0u;
   }
   // f and the weight 1 - f of the input
-  __device__ __forceinline__ void gates(int u, int k, uint32_t hold, float& f, float& in) const {
-    if constexpr (SIG) {
-      sigmoid2<T>(z[u].get(k), f, in);
-    } else {
-      f = z[u].get(k);
-      in = 1.0f;
+  __device__ __forceinline__ void gates(int u, uint32_t hold, float* f, float* in) const {
+#pragma unroll
+    for (int k = 0; k < V; ++k) {
+      if constexpr (SIG) {
+        sigmoid2<T>(z[u].get(k), f[k], in[k]);
+      } else {
+        f[k] = z[u].get(k);
+        in[k] = 1.0f;
+      }
     }
-    if (MASK && (hold >> k & 1u)) {
-      f = 1.0f;
-      in = 0.0f;
+    if (MASK && any_lane(hold)) {
+#pragma unroll
+      for (int k = 0; k < V; ++k)
+        if (hold >> k & 1u) f[k] = 1.0f, in[k] = 0.0f;
+    }
+  }
+  // one step earlier in a range's (P, S)
+  __device__ __forceinline__ void prepend(int u, const float* f, uint32_t done, float* P, float* S) const {
+    if (MASK && any_lane(done)) {
+#pragma unroll
+      for (int k = 0; k < V; ++k)
+        if (done >> k & 1u) P[k] = 1.0f, S[k] = 0.0f;
+    }
+#pragma unroll
+    for (int k = 0; k < V; ++k) {
+      P[k] *= f[k];
+      S[k] = f[k] * (dh[u].get(k) + S[k]);
     }
   }
 };
 
 // (P, S) of every chunk of steps but the first
 template <class T, int V, bool SIG, bool MASK, bool NI>
-__global__ __launch_bounds__(1024) void k_scan_grad_ranges(ScanArgs a) {
-  constexpr int U = scan_steps<V>();
+__global__ __launch_bounds__(64 * SCAN_WAVES) void k_scan_grad_ranges(ScanArgs a) {
+  constexpr int U = scan_grad_steps<V>();
   extern __shared__ float lds[];   // [W][V][2][64]
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), W = blockDim.x >> 6;
   const Columns<V, NI> col(a, blockIdx.x, lane);
@@ -73,14 +91,9 @@ __global__ __launch_bounds__(1024) void k_scan_grad_ranges(ScanArgs a) {
       if (t0 + u < te) {
         uint32_t done = 0, hold = 0;
         if constexpr (MASK) st.masks(a, col, len, u, t0 + u, done, hold);
-#pragma unroll
-        for (int k = 0; k < V; ++k) {
-          float f, in;
-          st.gates(u, k, hold, f, in);
-          if (MASK && (done >> k & 1u)) P[k] = 1.0f, S[k] = 0.0f;
-          P[k] *= f;
-          S[k] = f * (st.dh[u].get(k) + S[k]);
-        }
+        float f[V], in[V];
+        st.gates(u, hold, f, in);
+        st.prepend(u, f, done, P, S);
         cut |= done;
       }
     }
@@ -93,9 +106,31 @@ __global__ __launch_bounds__(1024) void k_scan_grad_ranges(ScanArgs a) {
   put_range<V>(a.agg + ((int64_t)chunk * a.tiles + blockIdx.x) * 128 * V, lane, P, S);
 }
 
+// The same with what the results need besides: the input and the output of the step before
+template <class T, int V, int U, bool SIG, bool MASK, bool NI>
+struct BackwardRound : BackwardSteps<T, V, U, SIG, MASK, NI> {
+  Vec<T, V> x[U], hb[U];
+  typename Columns<V, NI>::Flags db;   // done of the step before the first
+
+  __device__ __forceinline__ void load(const ScanArgs& a, const Columns<V, NI>& col, const T* gate, const T* dout,
+                                       const T* in, const T* h, int t0, int tend) {
+    BackwardSteps<T, V, U, SIG, MASK, NI>::load(a, col, gate, dout, t0, tend);
+    const T *px = in + t0 * a.x.st, *ph = h + (t0 - 1) * a.h.st;
+#pragma unroll
+    for (int u = 0; u < U; ++u, px += a.x.st, ph += a.h.st) {
+      if (t0 + u < tend) {
+        if constexpr (SIG) x[u].load(px);
+        if (t0 + u > 0) hb[u].load(ph);
+      }
+    }
+    if constexpr (MASK)
+      if (a.done && t0 > 0 && t0 < tend) db = col.load_done(a, t0 - 1);
+  }
+};
+
 template <class T, int V, bool SIG, bool MASK, bool NI>
-__global__ __launch_bounds__(1024) void k_scan_backward(ScanArgs a) {
-  constexpr int U = scan_steps<V>();
+__global__ __launch_bounds__(64 * SCAN_WAVES) void k_scan_backward(ScanArgs a) {
+  constexpr int U = scan_grad_steps<V>();
   extern __shared__ float lds[];   // [2][W][V][2][64], by round parity
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), W = blockDim.x >> 6;
   const Columns<V, NI> col(a, blockIdx.x, lane);
@@ -122,23 +157,16 @@ __global__ __launch_bounds__(1024) void k_scan_backward(ScanArgs a) {
     for (int w = 0; w < W; ++w) run_range<V>(lds + (W + w) * 128 * V, lane, G);
   }
 
-  int parity = 0;
+  // the next round's loads are in flight while a round is computed
   const int span = W * U;
-  for (int r0 = tb + (te - tb - 1) / span * span; r0 >= tb; r0 -= span, parity ^= 1) {
+  const int first = tb + (te - tb - 1) / span * span;
+  BackwardRound<T, V, U, SIG, MASK, NI> next;
+  next.load(a, col, gate, dout, in, hp, first + wave * U, te);
+  int parity = 0;
+  for (int r0 = first; r0 >= tb; r0 -= span, parity ^= 1) {
     const int t0 = r0 + wave * U;
-    BackwardSteps<T, V, U, SIG, MASK, NI> st;
-    st.load(a, col, gate, dout, t0, te);
-    Vec<T, V> x[U], hb[U];      // the input, the output of the step before
-    typename Columns<V, NI>::Flags db{};   // done of the step before t0
-#pragma unroll
-    for (int u = 0; u < U; ++u) {
-      if (t0 + u < te) {
-        if constexpr (SIG) x[u].load(in + (int64_t)(t0 + u) * a.x.st);
-        if (t0 + u > 0) hb[u].load(hp + (int64_t)(t0 + u - 1) * a.h.st);
-      }
-    }
-    if constexpr (MASK)
-      if (a.done && t0 > 0 && t0 < te) db = col.load_done(a, t0 - 1);
+    const BackwardRound<T, V, U, SIG, MASK, NI> st = next;
+    if (r0 > tb) next.load(a, col, gate, dout, in, hp, t0 - span, te);
     float f[U][V], w1[U][V];
     uint32_t done[U], hold[U];
 #pragma unroll
@@ -146,12 +174,10 @@ __global__ __launch_bounds__(1024) void k_scan_backward(ScanArgs a) {
       done[u] = hold[u] = 0;
       if (t0 + u < te) {
         if constexpr (MASK) st.masks(a, col, len, u, t0 + u, done[u], hold[u]);
-#pragma unroll
-        for (int k = 0; k < V; ++k) st.gates(u, k, hold[u], f[u][k], w1[u][k]);
+        st.gates(u, hold[u], f[u], w1[u]);
       } else {
 #pragma unroll
         for (int k = 0; k < V; ++k) f[u][k] = 1.0f, w1[u][k] = 0.0f;
-        st.dh[u].w = 0;
       }
     }
     float before[V];   // G before the round's first step
@@ -162,53 +188,61 @@ __global__ __launch_bounds__(1024) void k_scan_backward(ScanArgs a) {
       for (int k = 0; k < V; ++k) P[k] = 1.0f, S[k] = 0.0f;
 #pragma unroll
       for (int u = U - 1; u >= 0; --u) {
-#pragma unroll
-        for (int k = 0; k < V; ++k) {
-          if (MASK && (done[u] >> k & 1u)) P[k] = 1.0f, S[k] = 0.0f;
-          P[k] *= f[u][k];
-          S[k] = f[u][k] * (st.dh[u].get(k) + S[k]);
-        }
+        st.prepend(u, f[u], done[u], P, S);
         cut |= done[u];
       }
       mark_cut<V>(P, cut);
-      float* x_ = lds + parity * W * 128 * V;
-      put_range<V>(x_ + wave * 128 * V, lane, P, S);
+      float* x = lds + parity * W * 128 * V;
+      put_range<V>(x + wave * 128 * V, lane, P, S);
       __syncthreads();
-      for (int w = W - 1; w > wave; --w) run_range<V>(x_ + w * 128 * V, lane, G);
+      for (int w = W - 1; w > wave; --w) run_range<V>(x + w * 128 * V, lane, G);
 #pragma unroll
       for (int k = 0; k < V; ++k) before[k] = G[k];
-      for (int w = wave; w >= 0; --w) run_range<V>(x_ + w * 128 * V, lane, before);
+      for (int w = wave; w >= 0; --w) run_range<V>(x + w * 128 * V, lane, before);
     }
 #pragma unroll
     for (int u = U - 1; u >= 0; --u) {
       if (t0 + u < te) {
         const int t = t0 + u;
-        uint32_t fresh = 0;   // columns whose state before this step is a new episode's zero
-        if constexpr (MASK) {
-          if (u) fresh = done[u > 0 ? u - 1 : 0];
-          else if (a.done && t > 0) fresh = col.ended(db);
+        float sp[V], gz[V], gx[V];
+        if (t > 0) {
+#pragma unroll
+          for (int k = 0; k < V; ++k) sp[k] = st.hb[u].get(k);
+        } else {
+#pragma unroll
+          for (int k = 0; k < V; ++k) sp[k] = a.h0.p ? a.h0.p[col.state_at(a, a.h0, k)] : 0.0f;
         }
-        float gz[V], gx[V];
+        if constexpr (MASK) {
+          // columns whose state before this step is a new episode's zero
+          const uint32_t fresh = u ? done[u > 0 ? u - 1 : 0] : (a.done && t > 0 ? col.ended(st.db) : 0u);
+          if (any_lane(fresh | done[u])) {
+#pragma unroll
+            for (int k = 0; k < V; ++k) {
+              if (fresh >> k & 1u) sp[k] = 0.0f;
+              if (done[u] >> k & 1u) G[k] = 0.0f;
+            }
+          }
+        }
 #pragma unroll
         for (int k = 0; k < V; ++k) {
-          if (MASK && (done[u] >> k & 1u)) G[k] = 0.0f;
           const float g = st.dh[u].get(k) + G[k];
-          float sp;
-          if (t > 0) sp = MASK && (fresh >> k & 1u) ? 0.0f : hb[u].get(k);
-          else sp = a.h0.p ? a.h0.p[col.state_at(a, a.h0, k)] : 0.0f;
           if constexpr (SIG) {
             gx[k] = w1[u][k] * g;
-            gz[k] = f[u][k] * (sp - x[u].get(k)) * gx[k];
+            gz[k] = f[u][k] * (sp[k] - st.x[u].get(k)) * gx[k];
           } else {
             gx[k] = g;
-            gz[k] = sp * g;
+            gz[k] = sp[k] * g;
           }
-          if (MASK && (hold[u] >> k & 1u)) gx[k] = gz[k] = 0.0f;
           G[k] = f[u][k] * g;
         }
+        if (MASK && any_lane(hold[u])) {
+#pragma unroll
+          for (int k = 0; k < V; ++k)
+            if (hold[u] >> k & 1u) gx[k] = gz[k] = 0.0f;
+        }
         if (col.active) {
-          store_own<T, V>(dgate + (int64_t)t * a.dgate.st, gz, col.shift);
-          store_own<T, V>(dx + (int64_t)t * a.dx.st, gx, col.shift);
+          store_own<T, V>(dgate + t * a.dgate.st, gz, col.shift);
+          store_own<T, V>(dx + t * a.dx.st, gx, col.shift);
         }
       }
     }
