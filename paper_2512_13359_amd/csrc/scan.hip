@@ -78,11 +78,12 @@ __global__ __launch_bounds__(64 * SCAN_WAVES) void k_scan_ranges(ScanArgs a) {
   constexpr int U = scan_steps<V>();
   extern __shared__ float lds[];   // [W][V][2][64]
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), W = blockDim.x >> 6;
-  const Columns<V, NI> col(a, blockIdx.x, lane);
+  const Place at(a);
+  const Columns<V, NI> col(a, at.tile, lane);
   const T *gate = col.template base<T>(a.gate), *in = col.template base<T>(a.x);
   typename Columns<V, NI>::Lens len{};
   if constexpr (MASK) len = col.load_lens(a);
-  const int part = a.chunk / W, tb = blockIdx.y * a.chunk + wave * part, te = min(a.T, tb + part);
+  const int part = a.chunk / W, tb = at.chunk * a.chunk + wave * part, te = min(a.T, tb + part);
   float P[V], S[V];
 #pragma unroll
   for (int k = 0; k < V; ++k) P[k] = 1.0f, S[k] = 0.0f;
@@ -107,7 +108,7 @@ __global__ __launch_bounds__(64 * SCAN_WAVES) void k_scan_ranges(ScanArgs a) {
   __syncthreads();
   if (wave) return;
   for (int w = 1; w < W; ++w) join_range<V>(lds + w * 128 * V, lane, P, S);
-  put_range<V>(a.agg + ((int64_t)blockIdx.y * a.tiles + blockIdx.x) * 128 * V, lane, P, S);
+  put_range<V>(a.agg + ((int64_t)at.chunk * a.tiles + at.tile) * 128 * V, lane, P, S);
 }
 
 template <class T, int V, bool SIG, bool MASK, bool NI>
@@ -115,23 +116,24 @@ __global__ __launch_bounds__(64 * SCAN_WAVES) void k_scan_forward(ScanArgs a) {
   constexpr int U = scan_steps<V>();
   extern __shared__ float lds[];   // [2][W][V][2][64], by round parity
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), W = blockDim.x >> 6;
-  const Columns<V, NI> col(a, blockIdx.x, lane);
+  const Place at(a);
+  const Columns<V, NI> col(a, at.tile, lane);
   const T *gate = col.template base<T>(a.gate), *in = col.template base<T>(a.x);
   T* out = col.template base<T>(a.h);
   typename Columns<V, NI>::Lens len{};
   if constexpr (MASK) len = col.load_lens(a);
-  const int tb = blockIdx.y * a.chunk, te = min(a.T, tb + a.chunk);
+  const int tb = at.chunk * a.chunk, te = min(a.T, tb + a.chunk);
 
   float s[V];
 #pragma unroll
   for (int k = 0; k < V; ++k) s[k] = a.h0.p ? a.h0.p[col.state_at(a, a.h0, k)] : 0.0f;
-  if (blockIdx.y) {   // the chunks before this one, a part per wave
+  if (at.chunk) {   // the chunks before this one, a part per wave
     float P[V], S[V];
 #pragma unroll
     for (int k = 0; k < V; ++k) P[k] = 1.0f, S[k] = 0.0f;
-    const int j1 = (int)((int64_t)(wave + 1) * blockIdx.y / W);
-    for (int j = (int)((int64_t)wave * blockIdx.y / W); j < j1; ++j)
-      join_range<V>(a.agg + ((int64_t)j * a.tiles + blockIdx.x) * 128 * V, lane, P, S);
+    const int j1 = (int)((int64_t)(wave + 1) * at.chunk / W);
+    for (int j = (int)((int64_t)wave * at.chunk / W); j < j1; ++j)
+      join_range<V>(a.agg + ((int64_t)j * a.tiles + at.tile) * 128 * V, lane, P, S);
     put_range<V>(lds + (W + wave) * 128 * V, lane, P, S);
     __syncthreads();
     for (int w = 0; w < W; ++w) run_range<V>(lds + (W + w) * 128 * V, lane, s);
@@ -199,7 +201,7 @@ __global__ __launch_bounds__(64 * SCAN_WAVES) void k_scan_forward(ScanArgs a) {
       for (int k = 0; k < V; ++k) s[k] = end[k];
     }
   }
-  if (a.last.p && blockIdx.y == gridDim.y - 1 && wave == 0 && col.active) {
+  if (a.last.p && at.chunk == a.K - 1 && wave == 0 && col.active) {
 #pragma unroll
     for (int k = 0; k < V; ++k)
       if (k >= col.shift) a.last.p[col.state_at(a, a.last, k)] = s[k];
@@ -212,10 +214,10 @@ int launch_scan_forward(const ScanArgs& a, const ScanShape& sh, bool bf16, bool 
   void* args[1] = {&arg};
   const size_t range = sizeof(float) * 128 * sh.V;
   if (sh.K > 1)
-    if (int rc = launch_kernel("auv_scan_forward", AUV_SCAN_KERNEL(k_scan_ranges), dim3(a.tiles, sh.K - 1), dim3(64 * sh.W), args,
+    if (int rc = launch_kernel("auv_scan_forward", AUV_SCAN_KERNEL(k_scan_ranges), dim3(a.tiles * (sh.K - 1)), dim3(64 * sh.W), args,
                                sh.W * range, s))
       return rc;
-  return launch_kernel("auv_scan_forward", AUV_SCAN_KERNEL(k_scan_forward), dim3(a.tiles, sh.K), dim3(64 * sh.W), args,
+  return launch_kernel("auv_scan_forward", AUV_SCAN_KERNEL(k_scan_forward), dim3(a.tiles * sh.K), dim3(64 * sh.W), args,
                        2 * sh.W * range, s);
 }
 
@@ -316,6 +318,7 @@ static void scan_shape(const auv_scan* d, const auv_seq* const* seqs, int count,
   a.chunk = ((rounds - 1) / sh.K + 1) * span;
   sh.K = (d->T - 1) / a.chunk + 1;
   a.K = sh.K;
+  a.grouped = sh.K == 1 && d->x.st * (d->type == AUV_BF16 ? 2 : 4) % 128 != 0;
   a.T = d->T;
   a.n = n;
   a.c = c;

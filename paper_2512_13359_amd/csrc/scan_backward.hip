@@ -72,12 +72,13 @@ __global__ __launch_bounds__(64 * SCAN_WAVES) void k_scan_grad_ranges(ScanArgs a
   constexpr int U = scan_grad_steps<V>();
   extern __shared__ float lds[];   // [W][V][2][64]
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), W = blockDim.x >> 6;
-  const Columns<V, NI> col(a, blockIdx.x, lane);
+  const Place at(a);
+  const Columns<V, NI> col(a, at.tile, lane);
   const T* gate = col.template base<T>(a.gate);
   const T* dout = a.dout.p ? col.template base<T>(a.dout) : nullptr;
   typename Columns<V, NI>::Lens len{};
   if constexpr (MASK) len = col.load_lens(a);
-  const int chunk = blockIdx.y + 1;
+  const int chunk = at.chunk + 1;
   const int part = a.chunk / W, tb = chunk * a.chunk + wave * part, te = min(a.T, tb + part);
   float P[V], S[V];
 #pragma unroll
@@ -103,7 +104,7 @@ __global__ __launch_bounds__(64 * SCAN_WAVES) void k_scan_grad_ranges(ScanArgs a
   __syncthreads();
   if (wave != W - 1) return;
   for (int w = W - 2; w >= 0; --w) join_range<V>(lds + w * 128 * V, lane, P, S);
-  put_range<V>(a.agg + ((int64_t)chunk * a.tiles + blockIdx.x) * 128 * V, lane, P, S);
+  put_range<V>(a.agg + ((int64_t)chunk * a.tiles + at.tile) * 128 * V, lane, P, S);
 }
 
 // The same with what the results need besides: the input and the output of the step before
@@ -133,25 +134,26 @@ __global__ __launch_bounds__(64 * SCAN_WAVES) void k_scan_backward(ScanArgs a) {
   constexpr int U = scan_grad_steps<V>();
   extern __shared__ float lds[];   // [2][W][V][2][64], by round parity
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), W = blockDim.x >> 6;
-  const Columns<V, NI> col(a, blockIdx.x, lane);
+  const Place at(a);
+  const Columns<V, NI> col(a, at.tile, lane);
   const T *gate = col.template base<T>(a.gate), *in = col.template base<T>(a.x), *hp = col.template base<T>(a.h);
   const T* dout = a.dout.p ? col.template base<T>(a.dout) : nullptr;
   T *dgate = col.template base<T>(a.dgate), *dx = col.template base<T>(a.dx);
   typename Columns<V, NI>::Lens len{};
   if constexpr (MASK) len = col.load_lens(a);
-  const int tb = blockIdx.y * a.chunk, te = min(a.T, tb + a.chunk);
+  const int tb = at.chunk * a.chunk, te = min(a.T, tb + a.chunk);
 
   float G[V];
 #pragma unroll
   for (int k = 0; k < V; ++k) G[k] = a.last.p ? a.last.p[col.state_at(a, a.last, k)] : 0.0f;
-  const int later = a.K - 1 - (int)blockIdx.y;
+  const int later = a.K - 1 - at.chunk;
   if (later) {   // the chunks after this one, a part per wave
     float P[V], S[V];
 #pragma unroll
     for (int k = 0; k < V; ++k) P[k] = 1.0f, S[k] = 0.0f;
     const int j0 = (int)((int64_t)wave * later / W), j1 = (int)((int64_t)(wave + 1) * later / W);
     for (int j = j0; j < j1; ++j)   // from the last chunk down
-      join_range<V>(a.agg + ((int64_t)(a.K - 1 - j) * a.tiles + blockIdx.x) * 128 * V, lane, P, S);
+      join_range<V>(a.agg + ((int64_t)(a.K - 1 - j) * a.tiles + at.tile) * 128 * V, lane, P, S);
     put_range<V>(lds + (W + wave) * 128 * V, lane, P, S);
     __syncthreads();
     for (int w = 0; w < W; ++w) run_range<V>(lds + (W + w) * 128 * V, lane, G);
@@ -251,7 +253,7 @@ __global__ __launch_bounds__(64 * SCAN_WAVES) void k_scan_backward(ScanArgs a) {
       for (int k = 0; k < V; ++k) G[k] = before[k];
     }
   }
-  if (a.dh0.p && blockIdx.y == 0 && wave == 0 && col.active) {
+  if (a.dh0.p && at.chunk == 0 && wave == 0 && col.active) {
 #pragma unroll
     for (int k = 0; k < V; ++k)
       if (k >= col.shift) a.dh0.p[col.state_at(a, a.dh0, k)] = G[k];
@@ -264,10 +266,10 @@ int launch_scan_backward(const ScanArgs& a, const ScanShape& sh, bool bf16, bool
   void* args[1] = {&arg};
   const size_t range = sizeof(float) * 128 * sh.V;
   if (sh.K > 1)
-    if (int rc = launch_kernel("auv_scan_backward", AUV_SCAN_KERNEL(k_scan_grad_ranges), dim3(a.tiles, sh.K - 1),
+    if (int rc = launch_kernel("auv_scan_backward", AUV_SCAN_KERNEL(k_scan_grad_ranges), dim3(a.tiles * (sh.K - 1)),
                                dim3(64 * sh.W), args, sh.W * range, s))
       return rc;
-  return launch_kernel("auv_scan_backward", AUV_SCAN_KERNEL(k_scan_backward), dim3(a.tiles, sh.K), dim3(64 * sh.W), args,
+  return launch_kernel("auv_scan_backward", AUV_SCAN_KERNEL(k_scan_backward), dim3(a.tiles * sh.K), dim3(64 * sh.W), args,
                        2 * sh.W * range, s);
 }
 
