@@ -22,6 +22,8 @@ template <class T, int V> struct Vec {
 
   __device__ __forceinline__ void load(const T* p) { w = *reinterpret_cast<const decltype(w)*>(p); }
   __device__ __forceinline__ void store(T* p) const { *reinterpret_cast<decltype(w)*>(p) = w; }
+  // past the caches' use: what a launch writes once and does not read
+  __device__ __forceinline__ void stream(T* p) const { __builtin_nontemporal_store(w, reinterpret_cast<decltype(w)*>(p)); }
   __device__ __forceinline__ float get(int k) const {
     if constexpr (sizeof(T) == 4 && V == 1) return __uint_as_float(w);
     else if constexpr (sizeof(T) == 4) return __uint_as_float(w[k]);
@@ -60,11 +62,18 @@ template <class T> __device__ __forceinline__ T to_elem(float v) {
 
 // Stores the elements k >= shift of a vector whose first ones belong to its neighbour: rows of a
 // length that V does not divide end in a vector moved back to end with the row.
-template <class T, int V> __device__ __forceinline__ void store_own(T* p, const float* v, int shift) {
+// `shared`: rows share cache lines, whose parts are to meet in L2.
+template <class T, int V> __device__ __forceinline__ void store_own(T* p, const float* v, int shift, bool shared) {
   if (shift == 0) {
     Vec<T, V> r;
     r.set(v);
-    r.store(p);
+    if (shared) {   // kept apart from the other branch, or the two stores would be joined into one without the hint
+      asm volatile("");
+      r.store(p);
+      asm volatile("");
+    } else {
+      r.stream(p);
+    }
   } else {
 #pragma unroll
     for (int k = 1; k < V; ++k)
@@ -117,7 +126,7 @@ template <class T> __device__ __forceinline__ float act_of(int act, float u) {
   if (act == ACT_SILU) {
     float f, g;
     sigmoid2<T>(u, f, g);
-    return u == -INFINITY ? 0.0f : u * f;
+    return u * f;
   }
   if (act == ACT_TANH) return tanh_of<T>(u);
   return u;
@@ -137,6 +146,34 @@ template <class T> __device__ __forceinline__ float act_slope(int act, float u) 
     return 4.0f * e * r * r;
   }
   return 1.0f;
+}
+
+// u <- act(u), u <- act'(u) for M values: one choice for all
+template <class T, int M> __device__ __forceinline__ void act_all(int act, float* u) {
+  auto each = [&](int which) {
+#pragma unroll
+    for (int k = 0; k < M; ++k) u[k] = act_of<T>(which, u[k]);
+  };
+  if (act == ACT_RELU) each(ACT_RELU);
+  else if (act == ACT_SILU) each(ACT_SILU);
+  else if (act == ACT_TANH) each(ACT_TANH);
+}
+template <class T, int M> __device__ __forceinline__ void slope_all(int act, float* u) {
+  auto each = [&](int which) {
+#pragma unroll
+    for (int k = 0; k < M; ++k) u[k] = act_slope<T>(which, u[k]);
+  };
+  if (act == ACT_RELU) each(ACT_RELU);
+  else if (act == ACT_SILU) each(ACT_SILU);
+  else if (act == ACT_TANH) each(ACT_TANH);
+  else each(ACT_NONE);
+}
+
+// 1 / sqrt(v): the instruction (one ulp) and a Newton step, far from the ends of the range
+__device__ __forceinline__ float rsqrt_of(float v) {
+  if (!(v > 1e-30f && v < 1e30f)) return 1.0f / sqrtf(v);
+  const float r = __builtin_amdgcn_rsqf(v);
+  return __builtin_fmaf(r * 0.5f, __builtin_fmaf(-v * r, r, 1.0f), r);
 }
 
 }  // namespace auv

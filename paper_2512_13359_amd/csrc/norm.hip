@@ -28,8 +28,23 @@ struct NormArgs {
   DropArgs drop;
 };
 
+// Sum over a team of 1 to 64 lanes (a power of two), every lane gets it: moves within rows of 16
+// lanes, then lane swaps.
 __device__ __forceinline__ float team_sum(float v, int lanes) {
-  for (int d = 1; d < lanes; d <<= 1) v += __shfl_xor(v, d);
+  if (lanes > 1) v += dpp_move<DPP_QUAD_SWAP1>(v);
+  if (lanes > 2) v += dpp_move<DPP_QUAD_SWAP2>(v);
+  if (lanes > 4) v += dpp_move<DPP_ROW_HALF_MIRROR>(v);   // the other quad of eight lanes, equal in its four
+  if (lanes > 8) v += dpp_move<DPP_ROW_MIRROR>(v);
+  if (lanes > 16) {
+    float u = v;
+    asm("s_nop 1\n\tv_permlane16_swap_b32 %0, %1" : "+v"(v), "+v"(u));
+    v += u;
+  }
+  if (lanes > 32) {
+    float u = v;
+    asm("s_nop 1\n\tv_permlane32_swap_b32 %0, %1" : "+v"(v), "+v"(u));
+    v += u;
+  }
   return v;
 }
 
@@ -75,7 +90,9 @@ __global__ __launch_bounds__(256) void k_norm_rows(NormArgs a) {
   const int per = 256 / a.lanes;
   const int64_t rows = (int64_t)a.n * a.G, stride = (int64_t)gridDim.x * per;   // a multiple of G
   int64_t r = (int64_t)blockIdx.x * per + tm.team;
-  const int g = (int)(r % a.G);
+  const int g = a.G == 1 ? 0 : (int)(r % a.G);
+  int64_t sample = a.G == 1 ? r : r / a.G;
+  const int64_t samples = a.G == 1 ? stride : stride / a.G;
   float w[NV][V], b[NV][V];
 #pragma unroll
   for (int j = 0; j < NV; ++j)
@@ -86,13 +103,22 @@ __global__ __launch_bounds__(256) void k_norm_rows(NormArgs a) {
       b[j][k] = a.b ? a.b[c] : 0.0f;
     }
   const float inv = 1.0f / (float)a.m;
-  for (; r < rows; r += stride) {
-    const int64_t sample = a.G == 1 ? r : r / a.G;
-    const T* x = reinterpret_cast<const T*>(a.x) + sample * a.x_sn + g * a.m;
-    T* y = reinterpret_cast<T*>(a.y) + sample * a.y_sn + g * a.m;
+  const T* x = reinterpret_cast<const T*>(a.x) + sample * a.x_sn + g * a.m;
+  T* y = reinterpret_cast<T*>(a.y) + sample * a.y_sn + g * a.m;
+  Vec<T, V> next[NV];
+  if (r < rows) {
+#pragma unroll
+    for (int j = 0; j < NV; ++j) next[j].load(x + tm.at[j]);
+  }
+  for (; r < rows; r += stride, sample += samples, y += samples * a.y_sn) {
     Vec<T, V> q[NV];
 #pragma unroll
-    for (int j = 0; j < NV; ++j) q[j].load(x + tm.at[j]);
+    for (int j = 0; j < NV; ++j) q[j] = next[j];
+    x += samples * a.x_sn;
+    if (r + stride < rows) {
+#pragma unroll
+      for (int j = 0; j < NV; ++j) next[j].load(x + tm.at[j]);
+    }
     float v[NV][V], sum = 0.0f;
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
@@ -114,14 +140,14 @@ __global__ __launch_bounds__(256) void k_norm_rows(NormArgs a) {
         v[j][k] -= mean;
         if (k >= tm.shift[j]) ss = __builtin_fmaf(v[j][k], v[j][k], ss);
       }
-    const float rstd = 1.0f / sqrtf(__builtin_fmaf(team_sum(ss, a.lanes), inv, a.eps));
+    const float rstd = rsqrt_of(__builtin_fmaf(team_sum(ss, a.lanes), inv, a.eps));
 #pragma unroll
-    for (int j = 0; j < NV; ++j) {
-      float o[V];
+    for (int j = 0; j < NV; ++j)
 #pragma unroll
-      for (int k = 0; k < V; ++k) o[k] = act_of<T>(a.act, __builtin_fmaf(v[j][k] * rstd, w[j][k], b[j][k]));
-      store_own<T, V>(y + tm.at[j], o, tm.shift[j]);
-    }
+      for (int k = 0; k < V; ++k) v[j][k] = __builtin_fmaf(v[j][k] * rstd, w[j][k], b[j][k]);
+    act_all<T, NV * V>(a.act, &v[0][0]);
+#pragma unroll
+    for (int j = 0; j < NV; ++j) store_own<T, V>(y + tm.at[j], v[j], tm.shift[j], false);
     if (tm.lane == 0) {
       a.mean[r] = mean;
       a.rstd[r] = rstd;
@@ -135,8 +161,9 @@ __global__ __launch_bounds__(256) void k_norm_rows_grad(NormArgs a) {
   const int per = 256 / a.lanes;
   const int64_t rows = (int64_t)a.n * a.G, stride = (int64_t)gridDim.x * per;   // a multiple of G
   int64_t r = (int64_t)blockIdx.x * per + tm.team;
-  const int64_t first = r;
-  const int g = (int)(r % a.G);
+  const int g = a.G == 1 ? 0 : (int)(r % a.G);
+  int64_t sample = a.G == 1 ? r : r / a.G;
+  const int64_t samples = a.G == 1 ? stride : stride / a.G, first = sample;
   float w[NV][V], b[NV][V], dw[NV][V], db[NV][V];
 #pragma unroll
   for (int j = 0; j < NV; ++j)
@@ -148,18 +175,29 @@ __global__ __launch_bounds__(256) void k_norm_rows_grad(NormArgs a) {
       dw[j][k] = db[j][k] = 0.0f;
     }
   const float inv = 1.0f / (float)a.m;
-  for (; r < rows; r += stride) {
-    const int64_t sample = a.G == 1 ? r : r / a.G;
-    const T* x = reinterpret_cast<const T*>(a.x) + sample * a.x_sn + g * a.m;
-    const T* dy = reinterpret_cast<const T*>(a.dout) + sample * a.dout_sn + g * a.m;
-    T* dx = reinterpret_cast<T*>(a.dx) + sample * a.dx_sn + g * a.m;
-    Vec<T, V> q[NV], e[NV];
+  const T* x = reinterpret_cast<const T*>(a.x) + sample * a.x_sn + g * a.m;
+  const T* dy = reinterpret_cast<const T*>(a.dout) + sample * a.dout_sn + g * a.m;
+  T* dx = reinterpret_cast<T*>(a.dx) + sample * a.dx_sn + g * a.m;
+  Vec<T, V> next_x[NV], next_e[NV];
+  float next_mean = 0.0f, next_rstd = 0.0f;
+  auto load = [&](int64_t row) {
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
-      q[j].load(x + tm.at[j]);
-      e[j].load(dy + tm.at[j]);
+      next_x[j].load(x + tm.at[j]);
+      next_e[j].load(dy + tm.at[j]);
     }
-    const float mean = a.mean[r], rstd = a.rstd[r];
+    next_mean = a.mean[row];
+    next_rstd = a.rstd[row];
+  };
+  if (r < rows) load(r);
+  for (; r < rows; r += stride, sample += samples, dx += samples * a.dx_sn) {
+    Vec<T, V> q[NV], e[NV];
+#pragma unroll
+    for (int j = 0; j < NV; ++j) q[j] = next_x[j], e[j] = next_e[j];
+    const float mean = next_mean, rstd = next_rstd;
+    x += samples * a.x_sn;
+    dy += samples * a.dout_sn;
+    if (r + stride < rows) load(r + stride);
     float xh[NV][V], d[NV][V], s1 = 0.0f, s2 = 0.0f;
     uint32_t keep[NV];
 #pragma unroll
@@ -171,7 +209,15 @@ __global__ __launch_bounds__(256) void k_norm_rows_grad(NormArgs a) {
         float v = q[j].get(k);
         if constexpr (DROP) v = keep[j] >> k & 1u ? v * a.drop.scale : 0.0f;
         xh[j][k] = (v - mean) * rstd;
-        float du = e[j].get(k) * act_slope<T>(a.act, __builtin_fmaf(xh[j][k], w[j][k], b[j][k]));
+        d[j][k] = __builtin_fmaf(xh[j][k], w[j][k], b[j][k]);
+      }
+    }
+    slope_all<T, NV * V>(a.act, &d[0][0]);
+#pragma unroll
+    for (int j = 0; j < NV; ++j)
+#pragma unroll
+      for (int k = 0; k < V; ++k) {
+        float du = e[j].get(k) * d[j][k];
         if (k < tm.shift[j]) du = 0.0f;
         dw[j][k] = __builtin_fmaf(du, xh[j][k], dw[j][k]);
         db[j][k] += du;
@@ -179,7 +225,6 @@ __global__ __launch_bounds__(256) void k_norm_rows_grad(NormArgs a) {
         s1 += d[j][k];
         s2 = __builtin_fmaf(d[j][k], xh[j][k], s2);
       }
-    }
     s1 = team_sum(s1, a.lanes) * inv;
     s2 = team_sum(s2, a.lanes) * inv;
 #pragma unroll
@@ -190,14 +235,14 @@ __global__ __launch_bounds__(256) void k_norm_rows_grad(NormArgs a) {
         o[k] = rstd * (d[j][k] - s1 - xh[j][k] * s2);
         if constexpr (DROP) o[k] = keep[j] >> k & 1u ? o[k] * a.drop.scale : 0.0f;
       }
-      store_own<T, V>(dx + tm.at[j], o, tm.shift[j]);
+      store_own<T, V>(dx + tm.at[j], o, tm.shift[j], false);
     }
   }
   if (!a.part) return;
   // [part row][2][channels]: a team's own sums where there are several groups (team t holds group
   // t mod G), else the workgroup's
   if (a.G > 1) {
-    float* p = a.part + first / a.G * 2 * a.C + g * a.m;
+    float* p = a.part + first * 2 * a.C + g * a.m;
 #pragma unroll
     for (int j = 0; j < NV; ++j)
 #pragma unroll
@@ -355,7 +400,7 @@ __global__ __launch_bounds__(256) void k_norm_stats_join(NormArgs a) {
   if (threadIdx.x == 0) {
     for (int w = 1; w < (int)blockDim.x / 64; ++w) join_moments(n, mean, M, sh[0][w], sh[1][w], sh[2][w]);
     a.mean[blockIdx.x] = mean;
-    a.rstd[blockIdx.x] = 1.0f / sqrtf(M / n + a.eps);
+    a.rstd[blockIdx.x] = rsqrt_of(M / n + a.eps);
   }
 }
 
@@ -389,9 +434,9 @@ __global__ __launch_bounds__(256) void k_norm_apply(NormArgs a) {
     for (int k = 0; k < V; ++k) v[k] = q.get(k);
     if constexpr (DROP) wk.dropped(a, s, v);
 #pragma unroll
-    for (int k = 0; k < V; ++k)
-      v[k] = act_of<T>(a.act, __builtin_fmaf((v[k] - ch.mean[k]) * ch.rstd[k], ch.w[k], ch.b[k]));
-    store_own<T, V>(y + s * a.y_ss, v, wk.shift);
+    for (int k = 0; k < V; ++k) v[k] = __builtin_fmaf((v[k] - ch.mean[k]) * ch.rstd[k], ch.w[k], ch.b[k]);
+    act_all<T, V>(a.act, v);
+    store_own<T, V>(y + s * a.y_ss, v, wk.shift, false);
   }
 }
 
@@ -410,15 +455,20 @@ __global__ __launch_bounds__(256) void k_norm_grad_sums(NormArgs a) {
       Vec<T, V> q, e;
       q.load(x + s * a.x_ss);
       e.load(dy + s * a.dout_ss);
-      float v[V];
+      float v[V], u[V];
 #pragma unroll
       for (int k = 0; k < V; ++k) v[k] = q.get(k);
       if constexpr (DROP) wk.dropped(a, s, v);
 #pragma unroll
       for (int k = 0; k < V; ++k) {
-        const float xh = (v[k] - ch.mean[k]) * ch.rstd[k];
-        const float du = e.get(k) * act_slope<T>(a.act, __builtin_fmaf(xh, ch.w[k], ch.b[k]));
-        dw[k] = __builtin_fmaf(du, xh, dw[k]);
+        v[k] = (v[k] - ch.mean[k]) * ch.rstd[k];
+        u[k] = __builtin_fmaf(v[k], ch.w[k], ch.b[k]);
+      }
+      slope_all<T, V>(a.act, u);
+#pragma unroll
+      for (int k = 0; k < V; ++k) {
+        const float du = e.get(k) * u[k];
+        dw[k] = __builtin_fmaf(du, v[k], dw[k]);
         db[k] += du;
       }
     }
@@ -492,23 +542,27 @@ __global__ __launch_bounds__(256) void k_norm_grad_apply(NormArgs a) {
     Vec<T, V> q, e;
     q.load(x + s * a.x_ss);
     e.load(dy + s * a.dout_ss);
-    float v[V];
+    float v[V], u[V];
     uint32_t keep = 0;
     if constexpr (DROP) keep = keep_from<V>(a.drop, (uint32_t)((int64_t)wk.i * a.S + s), wk.c);
 #pragma unroll
     for (int k = 0; k < V; ++k) {
       float xv = q.get(k);
       if constexpr (DROP) xv = keep >> k & 1u ? xv * a.drop.scale : 0.0f;
-      const float xh = (xv - ch.mean[k]) * ch.rstd[k];
-      const float du = e.get(k) * act_slope<T>(a.act, __builtin_fmaf(xh, ch.w[k], ch.b[k]));
-      v[k] = ch.rstd[k] * (du * ch.w[k] - m1[k] - xh * m2[k]);
+      v[k] = (xv - ch.mean[k]) * ch.rstd[k];
+      u[k] = __builtin_fmaf(v[k], ch.w[k], ch.b[k]);
+    }
+    slope_all<T, V>(a.act, u);
+#pragma unroll
+    for (int k = 0; k < V; ++k) {
+      v[k] = ch.rstd[k] * (e.get(k) * u[k] * ch.w[k] - m1[k] - v[k] * m2[k]);
       if constexpr (DROP) v[k] = keep >> k & 1u ? v[k] * a.drop.scale : 0.0f;
     }
-    store_own<T, V>(dx + s * a.dx_ss, v, wk.shift);
+    store_own<T, V>(dx + s * a.dx_ss, v, wk.shift, false);
   }
 }
 
-// dweight and dbias: the fixed-order sum of the partial rows [part_rows][2][S][C] (S = 1 but in the rows
+// dweight and dbias: the fixed-order sum of the partial rows [part_rows][2][S][C] (row r of S C: q = r / S, at q 2 S + r - q S = q S + r; S = 1 but in the rows
 // form of one group over several positions); 16 channels x 64 row lanes per workgroup.
 __global__ __launch_bounds__(1024) void k_norm_param_sum(NormArgs a, int S) {
   __shared__ float sh[64][17];
@@ -517,10 +571,12 @@ __global__ __launch_bounds__(1024) void k_norm_param_sum(NormArgs a, int S) {
   if (!out) return;
   float s = 0.0f;
   if (c < a.C) {
+    const float* p = a.part + blockIdx.y * (int64_t)S * a.C + c;
     const int64_t rows = (int64_t)a.part_rows * S;
+#pragma unroll 8
     for (int64_t r = lane; r < rows; r += 64) {
       const int64_t q = S == 1 ? r : r / S;
-      s += a.part[((2 * q + blockIdx.y) * S + (r - q * S)) * a.C + c];
+      s += p[(q * S + r) * a.C];
     }
   }
   sh[lane][col] = s;
@@ -587,7 +643,7 @@ __global__ __launch_bounds__(256) void k_dropout(DropoutArgs a) {
     for (int j = 0; j < NV; ++j) {
       Vec<T, V> q;
       q.set(v + j * V);
-      q.store(y + j * V);
+      q.stream(y + j * V);
     }
   } else {
 #pragma unroll

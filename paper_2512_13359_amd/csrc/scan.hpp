@@ -39,6 +39,7 @@ struct ScanArgs {
   int chunk;             // steps per workgroup, a multiple of W U (of U in the first launch)
   int K, tiles;
   bool grouped;   // neighbouring tiles on one XCD
+  bool shared;    // plain stores
 };
 
 __device__ __forceinline__ float smallest() { return __uint_as_float(1u); }

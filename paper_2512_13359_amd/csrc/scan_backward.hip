@@ -243,8 +243,8 @@ __global__ __launch_bounds__(64 * SCAN_WAVES) void k_scan_backward(ScanArgs a) {
             if (hold[u] >> k & 1u) gx[k] = gz[k] = 0.0f;
         }
         if (col.active) {
-          store_own<T, V>(dgate + t * a.dgate.st, gz, col.shift);
-          store_own<T, V>(dx + t * a.dx.st, gx, col.shift);
+          store_own<T, V>(dgate + t * a.dgate.st, gz, col.shift, a.shared);
+          store_own<T, V>(dx + t * a.dx.st, gx, col.shift, a.shared);
         }
       }
     }
