@@ -16,7 +16,7 @@ CSRC = os.path.join(HERE, "csrc")
 INCLUDE = os.path.join(os.path.dirname(HERE), "include")
 LIB = os.path.join(HERE, "libauv.so")
 SOURCES = ["auv_env.hip", "auv_policy.hip", "ppo.hip", "shac.hip", "rate_probe.hip", "scan.hip", "scan_backward.hip",
-           "norm.hip"]
+           "norm.hip", "norm_rows.hip", "dropout.hip"]
 
 HIPCC_FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC",

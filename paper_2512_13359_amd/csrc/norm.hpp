@@ -1,0 +1,62 @@
+// Group norm: what its three forms share.
+//   rows    a group is up to 1024 contiguous numbers (one position, or one group over dense positions): in the registers
+//           of 1 to 64 lanes (norm_rows.hip)
+//   block   a sample is up to a few thousand vectors: in the registers of a workgroup (norm.hip)
+//   chunks  larger samples: statistics by one launch, applied by the next, which reads the sample again (norm.hip)
+#pragma once
+
+#include "dropout.hpp"
+#include "layers.hpp"
+
+namespace auv {
+
+struct NormArgs {
+  char *x, *y, *dout, *dx;
+  int64_t x_sn, x_ss, y_sn, y_ss, dout_sn, dout_ss, dx_sn, dx_ss;
+  const float *w, *b;
+  float *mean, *rstd;
+  float* part;    // backward: rows of partial sums of dw and db, [2][channels] each
+  float* groups;  // chunk form: [n][chunk][tile][G][2] moments (forward) or sums of d and d xhat (backward)
+  float *dw, *db;
+  float eps;
+  int act, n, S, C, G, Cg;
+  int m, lanes;      // rows form: elements of a group, lanes per group
+  int tile, tiles;   // vectors of a row per workgroup, workgroups across it
+  int step, pack;    // block form: positions per pass, samples per pass
+  int chunks, per;   // chunk form: chunks of `per` positions
+  int part_rows;
+  DropArgs drop;
+};
+
+// Form and launch shape of a call.
+enum NormForm { NORM_ROWS, NORM_BLOCK, NORM_CHUNKS };
+struct NormPlan {
+  NormForm form;
+  int V, R, blocks, threads;   // vector; vectors per lane (rows) or thread (block); workgroups of the launch and their size
+  int m, lanes, tile, tiles, step, pack, chunks, per;
+  int64_t part_rows, width;    // backward: partial rows of [2][width] floats
+};
+
+// Sum over a team of 1 to 64 lanes (a power of two), every lane gets it: moves within rows of 16
+// lanes, then lane swaps.
+__device__ __forceinline__ float team_sum(float v, int lanes) {
+  if (lanes > 1) v += dpp_move<DPP_QUAD_SWAP1>(v);
+  if (lanes > 2) v += dpp_move<DPP_QUAD_SWAP2>(v);
+  if (lanes > 4) v += dpp_move<DPP_ROW_HALF_MIRROR>(v);   // the other quad of eight lanes, equal in its four
+  if (lanes > 8) v += dpp_move<DPP_ROW_MIRROR>(v);
+  if (lanes > 16) {
+    float u = v;
+    asm("s_nop 1\n\tv_permlane16_swap_b32 %0, %1" : "+v"(v), "+v"(u));
+    v += u;
+  }
+  if (lanes > 32) {
+    float u = v;
+    asm("s_nop 1\n\tv_permlane32_swap_b32 %0, %1" : "+v"(v), "+v"(u));
+    v += u;
+  }
+  return v;
+}
+
+int launch_norm_rows(const char* fn, const NormArgs& a, const NormPlan& p, bool bf16, bool grad, size_t lds, hipStream_t s);
+
+}  // namespace auv

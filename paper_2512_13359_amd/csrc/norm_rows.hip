@@ -1,0 +1,267 @@
+// Group norm, rows form (kernels).
+#include "norm.hpp"
+
+namespace auv {
+
+// A group of up to 1024 contiguous numbers (S = 1, or one group over dense positions) held in the
+// registers of 1 to 64 lanes: read once, statistics by lane swaps, written once.  A team of lanes
+// keeps its channels over all of its rows, and with them weights and the sums of their gradients.
+template <class T, int V, int NV> struct RowTeam {
+  int lane, team, at[NV], shift[NV];
+
+  __device__ __forceinline__ explicit RowTeam(const NormArgs& a) {
+    lane = threadIdx.x & (a.lanes - 1);
+    team = threadIdx.x / a.lanes;
+#pragma unroll
+    for (int j = 0; j < NV; ++j) {
+      const int e0 = (j * a.lanes + lane) * V;
+      at[j] = min(e0, a.m - V);
+      shift[j] = min(e0 - at[j], V);
+    }
+  }
+  __device__ __forceinline__ int channel(const NormArgs& a, int g, int j, int k) const {
+    return a.S == 1 ? g * a.m + at[j] + k : (at[j] + k) % a.C;
+  }
+  // the draws of a row's vector j
+  __device__ __forceinline__ void draw(const NormArgs& a, int64_t sample, int g, int j, Draws<V>& keep) const {
+    if (a.S == 1) {
+      keep.draw(a.drop, (uint32_t)sample, g * a.m + at[j]);
+      return;
+    }
+    uint32_t bits = 0;   // the vector may go over several positions
+    int pos = at[j] / a.C, c = at[j] % a.C;
+    for (int k = 0; k < V;) {
+      const int run = min(V - k, min(a.C - c, 8 - (c & 7)));
+      bits |= (drop_bits(a.drop, (uint32_t)(sample * a.S + pos), c >> 3) >> (c & 7) & ((1u << run) - 1u)) << k;
+      k += run;
+      c += run;
+      if (c == a.C) ++pos, c = 0;
+    }
+    keep.set(bits);
+  }
+};
+
+template <class T, int V, int NV, bool DROP, bool FULL>
+__global__ __launch_bounds__(256) void k_norm_rows(NormArgs a) {
+  constexpr bool full = FULL;   // every lane's vectors are whole and its own
+  const RowTeam<T, V, NV> tm(a);
+  const int per = 256 / a.lanes;
+  const int64_t rows = (int64_t)a.n * a.G, stride = (int64_t)gridDim.x * per;   // a multiple of G
+  int64_t r = (int64_t)blockIdx.x * per + tm.team;
+  const int g = a.G == 1 ? 0 : (int)(r % a.G);
+  int64_t sample = a.G == 1 ? r : r / a.G;
+  const int64_t samples = a.G == 1 ? stride : stride / a.G;
+  float w[NV][V], b[NV][V];
+#pragma unroll
+  for (int j = 0; j < NV; ++j)
+#pragma unroll
+    for (int k = 0; k < V; ++k) {
+      const int c = tm.channel(a, g, j, k);
+      w[j][k] = a.w ? a.w[c] : 1.0f;
+      b[j][k] = a.b ? a.b[c] : 0.0f;
+    }
+  const float inv = 1.0f / (float)a.m;
+  const T* x = reinterpret_cast<const T*>(a.x) + sample * a.x_sn + g * a.m;
+  T* y = reinterpret_cast<T*>(a.y) + sample * a.y_sn + g * a.m;
+  Vec<T, V> next[NV];
+  if (r < rows) {
+#pragma unroll
+    for (int j = 0; j < NV; ++j) next[j].load(x + tm.at[j]);
+  }
+  for (; r < rows; r += stride, sample += samples, y += samples * a.y_sn) {
+    Vec<T, V> q[NV];
+#pragma unroll
+    for (int j = 0; j < NV; ++j) q[j] = next[j];
+    x += samples * a.x_sn;
+    if (r + stride < rows) {
+#pragma unroll
+      for (int j = 0; j < NV; ++j) next[j].load(x + tm.at[j]);
+    }
+    float v[NV][V], sum = 0.0f;
+#pragma unroll
+    for (int j = 0; j < NV; ++j) {
+      // kept values enter unscaled: mean and deviations are scaled instead
+      Draws<V> keep;
+      if constexpr (DROP) tm.draw(a, sample, g, j, keep);
+#pragma unroll
+      for (int k = 0; k < V; ++k) {
+        v[j][k] = q[j].get(k);
+        if constexpr (DROP) v[j][k] = keep.kept(a.drop, k) ? v[j][k] : 0.0f;
+      }
+    }
+#pragma unroll
+    for (int j = 0; j < NV; ++j)
+#pragma unroll
+      for (int k = 0; k < V; ++k) sum += full || k >= tm.shift[j] ? v[j][k] : 0.0f;
+    const float mean = team_sum(sum, a.lanes) * inv;
+    float ss = 0.0f;
+#pragma unroll
+    for (int j = 0; j < NV; ++j)
+#pragma unroll
+      for (int k = 0; k < V; ++k) {
+        v[j][k] -= mean;
+        const float d = full || k >= tm.shift[j] ? v[j][k] : 0.0f;
+        ss = __builtin_fmaf(d, d, ss);
+      }
+    const float rstd = rsqrt_of(__builtin_fmaf(team_sum(ss, a.lanes), inv * a.drop.scale * a.drop.scale, a.eps));
+    const float f = rstd * a.drop.scale;
+#pragma unroll
+    for (int j = 0; j < NV; ++j)
+#pragma unroll
+      for (int k = 0; k < V; ++k) v[j][k] = __builtin_fmaf(v[j][k] * f, w[j][k], b[j][k]);
+    act_all<T, NV * V>(a.act, &v[0][0]);
+#pragma unroll
+    for (int j = 0; j < NV; ++j) store_own<T, V>(y + tm.at[j], v[j], full ? 0 : tm.shift[j], false);
+    if (tm.lane == 0) {
+      a.mean[r] = mean * a.drop.scale;
+      a.rstd[r] = rstd;
+    }
+  }
+}
+
+template <class T, int V, int NV, bool DROP, bool FULL>
+__global__ __launch_bounds__(256) void k_norm_rows_grad(NormArgs a) {
+  constexpr bool full = FULL;   // every lane's vectors are whole and its own
+  const RowTeam<T, V, NV> tm(a);
+  const int per = 256 / a.lanes;
+  const int64_t rows = (int64_t)a.n * a.G, stride = (int64_t)gridDim.x * per;   // a multiple of G
+  int64_t r = (int64_t)blockIdx.x * per + tm.team;
+  const int g = a.G == 1 ? 0 : (int)(r % a.G);
+  int64_t sample = a.G == 1 ? r : r / a.G;
+  const int64_t samples = a.G == 1 ? stride : stride / a.G, first = sample;
+  float w[NV][V], b[NV][V], dw[NV][V], db[NV][V];
+#pragma unroll
+  for (int j = 0; j < NV; ++j)
+#pragma unroll
+    for (int k = 0; k < V; ++k) {
+      const int c = tm.channel(a, g, j, k);
+      w[j][k] = a.w ? a.w[c] : 1.0f;
+      b[j][k] = a.b ? a.b[c] : 0.0f;
+      dw[j][k] = db[j][k] = 0.0f;
+    }
+  const float inv = 1.0f / (float)a.m;
+  const T* x = reinterpret_cast<const T*>(a.x) + sample * a.x_sn + g * a.m;
+  const T* dy = reinterpret_cast<const T*>(a.dout) + sample * a.dout_sn + g * a.m;
+  T* dx = reinterpret_cast<T*>(a.dx) + sample * a.dx_sn + g * a.m;
+  Vec<T, V> next_x[NV], next_e[NV];
+  float next_mean = 0.0f, next_rstd = 0.0f;
+  auto load = [&](int64_t row) {
+#pragma unroll
+    for (int j = 0; j < NV; ++j) {
+      next_x[j].load(x + tm.at[j]);
+      next_e[j].load(dy + tm.at[j]);
+    }
+    next_mean = a.mean[row];
+    next_rstd = a.rstd[row];
+  };
+  if (r < rows) load(r);
+  for (; r < rows; r += stride, sample += samples, dx += samples * a.dx_sn) {
+    Vec<T, V> q[NV], e[NV];
+#pragma unroll
+    for (int j = 0; j < NV; ++j) q[j] = next_x[j], e[j] = next_e[j];
+    const float mean = next_mean, rstd = next_rstd;
+    x += samples * a.x_sn;
+    dy += samples * a.dout_sn;
+    if (r + stride < rows) load(r + stride);
+    float xh[NV][V], d[NV][V], s1 = 0.0f, s2 = 0.0f;
+    Draws<V> keep[NV];
+#pragma unroll
+    for (int j = 0; j < NV; ++j) {
+      if constexpr (DROP) tm.draw(a, sample, g, j, keep[j]);
+#pragma unroll
+      for (int k = 0; k < V; ++k) {
+        float v = q[j].get(k);
+        if constexpr (DROP) v = keep[j].kept(a.drop, k) ? v : 0.0f;
+        xh[j][k] = __builtin_fmaf(v, a.drop.scale, -mean) * rstd;
+        d[j][k] = __builtin_fmaf(xh[j][k], w[j][k], b[j][k]);
+      }
+    }
+    slope_all<T, NV * V>(a.act, &d[0][0]);
+#pragma unroll
+    for (int j = 0; j < NV; ++j)
+#pragma unroll
+      for (int k = 0; k < V; ++k) {
+        float du = e[j].get(k) * d[j][k];
+        if (!full && k < tm.shift[j]) du = 0.0f;
+        dw[j][k] = __builtin_fmaf(du, xh[j][k], dw[j][k]);
+        db[j][k] += du;
+        d[j][k] = du * w[j][k];
+        s1 += d[j][k];
+        s2 = __builtin_fmaf(d[j][k], xh[j][k], s2);
+      }
+    s1 = team_sum(s1, a.lanes) * inv;
+    s2 = team_sum(s2, a.lanes) * inv;
+    const float f = rstd * a.drop.scale;
+#pragma unroll
+    for (int j = 0; j < NV; ++j) {
+      float o[V];
+#pragma unroll
+      for (int k = 0; k < V; ++k) {
+        o[k] = f * (d[j][k] - s1 - xh[j][k] * s2);
+        if constexpr (DROP) o[k] = keep[j].kept(a.drop, k) ? o[k] : 0.0f;
+      }
+      store_own<T, V>(dx + tm.at[j], o, full ? 0 : tm.shift[j], false);
+    }
+  }
+  if (!a.part) return;
+  // [part row][2][channels]: a team's own sums where there are several groups (team t holds group
+  // t mod G), else the workgroup's
+  if (a.G > 1) {
+    float* p = a.part + first * 2 * a.C + g * a.m;
+#pragma unroll
+    for (int j = 0; j < NV; ++j)
+#pragma unroll
+      for (int k = 0; k < V; ++k)
+        if (k >= tm.shift[j]) {
+          p[tm.at[j] + k] = dw[j][k];
+          p[a.C + tm.at[j] + k] = db[j][k];
+        }
+    return;
+  }
+  extern __shared__ float red[];   // [waves][2][m]
+#pragma unroll
+  for (int j = 0; j < NV; ++j)
+#pragma unroll
+    for (int k = 0; k < V; ++k)
+      for (int s = a.lanes; s < 64; s <<= 1) {
+        dw[j][k] += __shfl_xor(dw[j][k], s);
+        db[j][k] += __shfl_xor(db[j][k], s);
+      }
+  const int wave = threadIdx.x >> 6;
+  if ((int)(threadIdx.x & 63) < a.lanes) {
+#pragma unroll
+    for (int j = 0; j < NV; ++j)
+#pragma unroll
+      for (int k = 0; k < V; ++k)
+        if (k >= tm.shift[j]) {
+          red[(2 * wave) * a.m + tm.at[j] + k] = dw[j][k];
+          red[(2 * wave + 1) * a.m + tm.at[j] + k] = db[j][k];
+        }
+  }
+  __syncthreads();
+  for (int i = threadIdx.x; i < 2 * a.m; i += 256) {
+    float s = 0.0f;
+    for (int q = 0; q < 4; ++q) s += red[2 * q * a.m + i];
+    a.part[(int64_t)blockIdx.x * 2 * a.m + i] = s;
+  }
+}
+
+#define AUV_ROWS_FULL(KERN, T, V, NV, D) (full ? (const void*)KERN<T, V, NV, D, true> : (const void*)KERN<T, V, NV, D, false>)
+#define AUV_ROWS_KERNEL(KERN, D)                                                                    \
+  (bf16 ? (p.V == 8 ? (p.R == 1 ? AUV_ROWS_FULL(KERN, __bf16, 8, 1, D) : AUV_ROWS_FULL(KERN, __bf16, 8, 2, D)) \
+                    : (const void*)KERN<__bf16, 1, 1, D, false>)                                    \
+        : (p.V == 4 ? (p.R == 1   ? AUV_ROWS_FULL(KERN, float, 4, 1, D)                             \
+                       : p.R == 2 ? AUV_ROWS_FULL(KERN, float, 4, 2, D)                             \
+                                  : AUV_ROWS_FULL(KERN, float, 4, 4, D))                            \
+                    : (const void*)KERN<float, 1, 1, D, false>))
+
+int launch_norm_rows(const char* fn, const NormArgs& a, const NormPlan& p, bool bf16, bool grad, size_t lds, hipStream_t s) {
+  const bool drop = a.drop.drop, full = a.m == p.R * a.lanes * p.V;
+  NormArgs arg = a;
+  void* args[1] = {&arg};
+  const void* k = grad ? (drop ? AUV_ROWS_KERNEL(k_norm_rows_grad, true) : AUV_ROWS_KERNEL(k_norm_rows_grad, false))
+                       : (drop ? AUV_ROWS_KERNEL(k_norm_rows, true) : AUV_ROWS_KERNEL(k_norm_rows, false));
+  return launch_kernel(fn, k, dim3(p.blocks), dim3(256), args, lds, s);
+}
+
+}  // namespace auv

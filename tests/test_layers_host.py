@@ -66,8 +66,7 @@ def _norm(A, **kw):
 @pytest.mark.parametrize("change, word", [
     (dict(n=0), ">= 1"), (dict(groups=0), ">= 1"), (dict(groups=3), "divide"), (dict(type=5), "type"), (dict(act=9), "activation"),
     (dict(eps=-1.0), "eps"), (dict(eps=float("nan")), "eps"), (dict(weight=P + 1), "aligned"), (dict(x=None), "x"),
-    (dict(x=P + 1), "aligned"), (dict(x_ss=-8), "negative"), (dict(mean=None), "NULL"), (dict(c=1 << 21, groups=1), "large"),
-    (dict(n=1 << 24, s=2, c=2, groups=2), "2^24")])
+    (dict(x=P + 1), "aligned"), (dict(x_ss=-8), "negative"), (dict(mean=None), "NULL"), (dict(c=1 << 21, groups=1), "large")])
 def test_norm_refuses(change, word):
     from paper_2512_13359_amd import _abi as A
     rc = A.lib.auv_norm_forward(_norm(A, **change), A.AuvRows(2 * P, 24, 8), P, None)
@@ -83,7 +82,12 @@ def test_norm_refuses_outputs_and_workspace():
                     (A.AuvRows(None, 24, 8), "NULL")):
         rc = A.lib.auv_norm_forward(_norm(A), y, P, None)
         assert rc == A.AUV_EINVAL and word in A.auv_last_error(), A.auv_last_error()
-    assert A.lib.auv_norm_forward(_norm(A), A.AuvRows(2 * P, 24, 8), None, None) == A.AUV_EINVAL and "work" in A.auv_last_error()
+    # small samples need no workspace forward, long ones do
+    assert A.auv_norm_work_bytes(_norm(A), False) == 0
+    long = _norm(A, s=5000, x_sn=40000)
+    assert A.auv_norm_work_bytes(long, False) > 0 and A.auv_norm_work_bytes(long, True) > 0
+    assert A.lib.auv_norm_forward(long, A.AuvRows(2 * P, 40000, 8), None, None) == A.AUV_EINVAL and "work" in A.auv_last_error()
+    assert A.lib.auv_norm_work_bytes(_norm(A, n=1 << 24, s=64, c=256), 1) == -1 and "2^24" in A.auv_last_error()
     for g, word in ((A.AuvNormGrad(2 * P, 24, 8, P, 24, 8), "input"), (A.AuvNormGrad(2 * P, 24, 8, 2 * P, 24, 8), "input"),
                     (A.AuvNormGrad(2 * P, 24, 8, 3 * P, 24, 8, 6 * P, 6 * P), "same"),
                     (A.AuvNormGrad(2 * P, 24, 8, 3 * P, 24, 8, 6 * P + 2, None), "aligned")):
