@@ -43,16 +43,25 @@ template <class T, int V, int R> struct BlockTeam {
   }
 };
 
-// Sums over the positions of each sample's channels: PLANES values per thread and channel in, columns [pack C] in LDS
-// out.  rows [pack step][C] and parts [threads] are LDS scratch.
+// Sums over the positions of each sample's columns, a value per thread and channel in, columns [pack][C] in LDS out; a column is
+// a channel, or (merged) a vector of channels of one group, [pack][C / V].  rows [pack step][columns of a sample] and
+// parts [threads] are LDS scratch.
 template <int V, class Team>
-__device__ __forceinline__ void column_sums(const NormArgs& a, const Team& tm, const float* v, float* rows, float* parts, float* cols) {
-  const int width = a.pack * a.C, threads = blockDim.x;
-  float* own = (a.step == 1 ? cols : rows) + tm.q * a.C + tm.c;
+__device__ __forceinline__ void column_sums(const NormArgs& a, const Team& tm, const float* v, bool merged, float* rows, float* parts,
+                                            float* cols) {
+  const int C = merged ? a.tile : a.C, width = a.pack * C, threads = blockDim.x;
+  float* own = (a.step == 1 ? cols : rows) + tm.q * C;
   if (tm.on) {
+    if (merged) {
+      float s = 0.0f;
 #pragma unroll
-    for (int k = 0; k < V; ++k)
-      if (k >= tm.shift) own[k] = v[k];
+      for (int k = 0; k < V; ++k) s += v[k];
+      own[tm.c / V] = s;
+    } else {
+#pragma unroll
+      for (int k = 0; k < V; ++k)
+        if (k >= tm.shift) own[tm.c + k] = v[k];
+    }
   }
   __syncthreads();
   if (a.step == 1) return;
@@ -60,10 +69,10 @@ __device__ __forceinline__ void column_sums(const NormArgs& a, const Team& tm, c
   if (segs > 1) {
     const int t = threadIdx.x, seg = t / width, i = t - seg * width;
     if (seg < segs) {
-      const int p = i / a.C;
-      const float* from = rows + (p * a.step) * a.C + (i - p * a.C);
+      const int p = i / C;
+      const float* from = rows + (p * a.step) * C + (i - p * C);
       float s = 0.0f;
-      for (int r = seg; r < a.step; r += segs) s += from[r * a.C];
+      for (int r = seg; r < a.step; r += segs) s += from[r * C];
       parts[t] = s;
     }
     __syncthreads();
@@ -74,10 +83,10 @@ __device__ __forceinline__ void column_sums(const NormArgs& a, const Team& tm, c
     }
   } else {
     for (int i = threadIdx.x; i < width; i += threads) {
-      const int p = i / a.C;
-      const float* from = rows + (p * a.step) * a.C + (i - p * a.C);
+      const int p = i / C;
+      const float* from = rows + (p * a.step) * C + (i - p * C);
       float s = 0.0f;
-      for (int r = 0; r < a.step; ++r) s += from[r * a.C];
+      for (int r = 0; r < a.step; ++r) s += from[r * C];
       cols[i] = s;
     }
   }
@@ -85,12 +94,13 @@ __device__ __forceinline__ void column_sums(const NormArgs& a, const Team& tm, c
 }
 
 // Per group of each sample: done(sample of the pass, group, sum of the group's columns) by one lane; a barrier after it.
-template <class Done> __device__ __forceinline__ void group_sums(const NormArgs& a, const float* cols, Done done) {
-  const int lanes = lanes_for(a.Cg), all = a.pack * a.G;
+template <int V, class Done>
+__device__ __forceinline__ void group_sums(const NormArgs& a, const float* cols, bool merged, Done done) {
+  const int Cg = merged ? a.Cg / V : a.Cg, lanes = lanes_for(Cg), all = a.pack * a.G;
   for (int t = threadIdx.x; t / lanes < all; t += blockDim.x) {
     const int i = t / lanes, l = t & (lanes - 1);   // group i of the pass: Cg columns from i Cg on
     float s = 0.0f;
-    for (int c = l; c < a.Cg; c += lanes) s += cols[i * a.Cg + c];
+    for (int c = l; c < Cg; c += lanes) s += cols[i * Cg + c];
     s = team_sum(s, lanes);
     if (l == 0) done(i, s);
   }
@@ -102,6 +112,7 @@ __global__ __launch_bounds__(512) void k_norm_block(NormArgs a) {
   extern __shared__ float lds[];
   const BlockTeam<T, V, R> tm(a);
   const int width = a.pack * a.C, all = a.pack * a.G;
+  const bool merged = a.Cg % V == 0;   // a thread's channels are of one group
   float *mean = lds, *rstd = mean + all, *cols = rstd + all, *parts = cols + width, *rows = parts + blockDim.x;
   float w[V], b[V];
   int g[V];
@@ -140,8 +151,8 @@ __global__ __launch_bounds__(512) void k_norm_block(NormArgs a) {
         for (int k = 0; k < V; ++k) sum[k] += value(r, k);
       }
     }
-    column_sums<V>(a, tm, sum, rows, parts, cols);
-    group_sums(a, cols, [&](int j, float s) { mean[j] = s * inv; });
+    column_sums<V>(a, tm, sum, merged, rows, parts, cols);
+    group_sums<V>(a, cols, merged, [&](int j, float s) { mean[j] = s * inv; });
     float m[V];
 #pragma unroll
     for (int k = 0; k < V; ++k) {
@@ -157,8 +168,8 @@ __global__ __launch_bounds__(512) void k_norm_block(NormArgs a) {
           sum[k] = __builtin_fmaf(d, d, sum[k]);
         }
       }
-    column_sums<V>(a, tm, sum, rows, parts, cols);
-    group_sums(a, cols, [&](int j, float s) {
+    column_sums<V>(a, tm, sum, merged, rows, parts, cols);
+    group_sums<V>(a, cols, merged, [&](int j, float s) {
       const float f = rsqrt_of(__builtin_fmaf(s, inv, a.eps));
       rstd[j] = f;
       if (first * a.G + j < (int64_t)a.n * a.G) {
@@ -191,6 +202,7 @@ __global__ __launch_bounds__(512) void k_norm_block_grad(NormArgs a) {
   extern __shared__ float lds[];
   const BlockTeam<T, V, R> tm(a);
   const int width = a.pack * a.C, all = a.pack * a.G;
+  const bool merged = a.Cg % V == 0;   // a thread's channels are of one group
   float *m1 = lds, *m2 = m1 + all, *cols = m2 + all, *parts = cols + width, *rows = parts + blockDim.x;
   float w[V], b[V], dw[V], db[V];
   int g[V];
@@ -257,10 +269,10 @@ __global__ __launch_bounds__(512) void k_norm_block_grad(NormArgs a) {
       s1[k] *= w[k];
       s2[k] *= w[k];
     }
-    column_sums<V>(a, tm, s1, rows, parts, cols);
-    group_sums(a, cols, [&](int j, float s) { m1[j] = s * inv; });
-    column_sums<V>(a, tm, s2, rows, parts, cols);
-    group_sums(a, cols, [&](int j, float s) { m2[j] = s * inv; });
+    column_sums<V>(a, tm, s1, merged, rows, parts, cols);
+    group_sums<V>(a, cols, merged, [&](int j, float s) { m1[j] = s * inv; });
+    column_sums<V>(a, tm, s2, merged, rows, parts, cols);
+    group_sums<V>(a, cols, merged, [&](int j, float s) { m2[j] = s * inv; });
     if (live) {
       T* dx = reinterpret_cast<T*>(a.dx) + i * a.dx_sn + tm.c;
       float c1[V], c2[V];
@@ -289,7 +301,7 @@ __global__ __launch_bounds__(512) void k_norm_block_grad(NormArgs a) {
   if (!a.part) return;
   // the workgroup's sums, [2][C]: over its samples as well
   for (int plane = 0; plane < 2; ++plane) {
-    column_sums<V>(a, tm, plane ? db : dw, rows, parts, cols);
+    column_sums<V>(a, tm, plane ? db : dw, false, rows, parts, cols);
     for (int c = threadIdx.x; c < a.C; c += blockDim.x) {
       float s = 0.0f;
       for (int p = 0; p < a.pack; ++p) s += cols[p * a.C + c];
@@ -399,7 +411,7 @@ __device__ __forceinline__ void walk(const Walker<T, V>& wk, const T* x, int64_t
 
 template <class T, int V, bool DROP>
 __global__ __launch_bounds__(256) void k_norm_stats(NormArgs a) {
-  extern __shared__ float red[];   // means and squares, [2][step][tile V], then joined in their first rows
+  extern __shared__ float red[];   // means and squares about them, [2][step][tile V]
   const Walker<T, V> wk(a);
   const int width = a.tile * V;
   float *means = red, *squares = red + wk.step * width;
@@ -439,24 +451,26 @@ __global__ __launch_bounds__(256) void k_norm_stats(NormArgs a) {
       }
   }
   __syncthreads();
-  for (int q = threadIdx.x; q < wk.local; q += 256) {
-    float n = 0.0f, mean = 0.0f, M = 0.0f;
-    for (int r = 0; r < wk.step; ++r) {
-      const int count = (wk.s1 - wk.s0 - r + wk.step - 1) / wk.step;
-      if (count > 0) join_moments(n, mean, M, (float)count, means[r * width + q], squares[r * width + q]);
-    }
-    means[q] = mean;
-    squares[q] = M;
-  }
-  __syncthreads();
-  const int lanes = lanes_for(min(a.Cg, wk.local));
-  for (int t = threadIdx.x; wk.g0 + t / lanes <= wk.g1; t += 256) {
+  // a group's mean, then its squares about it, over the tile's rows and channels of the group
+  const int groups = wk.g1 - wk.g0 + 1, whole = (wk.s1 - wk.s0) / wk.step, rest = (wk.s1 - wk.s0) % wk.step;
+  const int lanes = lanes_for(min(min(a.Cg, wk.local) * wk.step, groups >= 256 ? 1 : 256 / groups));
+  for (int t = threadIdx.x; t / lanes < groups; t += 256) {
     const int g = wk.g0 + t / lanes, l = t & (lanes - 1);
     int lo, hi;
     wk.channels_of(a, g, lo, hi);
-    float n = 0.0f, mean = 0.0f, M = 0.0f;
-    for (int q = lo + l; q < hi; q += lanes) join_moments(n, mean, M, (float)(wk.s1 - wk.s0), means[q], squares[q]);
-    join_lanes(n, mean, M, lanes);
+    const int wide = hi - lo, all = wide * wk.step;
+    float s = 0.0f, M = 0.0f;
+    for (int e = l; e < all; e += lanes) {
+      const int r = e / wide, q = lo + e - r * wide;
+      s = __builtin_fmaf((float)(whole + (r < rest)), means[r * width + q], s);
+    }
+    const float mean = team_sum(s, lanes) / ((float)(wk.s1 - wk.s0) * (float)wide);
+    for (int e = l; e < all; e += lanes) {
+      const int r = e / wide, q = lo + e - r * wide;
+      const float d = means[r * width + q] - mean;
+      M += __builtin_fmaf((float)(whole + (r < rest)) * d, d, squares[r * width + q]);
+    }
+    M = team_sum(M, lanes);
     if (l == 0) wk.share(a)[g] = make_float2(mean, M);
   }
 }
@@ -566,17 +580,23 @@ __global__ __launch_bounds__(256) void k_norm_grad_sums(NormArgs a) {
   }
   __syncthreads();
   float* out = a.part + (int64_t)blockIdx.x * 2 * a.C + wk.base;
-  for (int q = threadIdx.x; q < wk.local; q += 256) {
+  const int per = lanes_for(min(wk.step, wk.local >= 256 ? 1 : 256 / wk.local));   // lanes per channel
+  for (int t = threadIdx.x; t / per < wk.local; t += 256) {
+    const int q = t / per, l = t & (per - 1);
     float dw = 0.0f, db = 0.0f;
-    for (int r = 0; r < wk.step; ++r) {
+    for (int r = l; r < wk.step; r += per) {
       dw += dws[r * width + q];
       db += dbs[r * width + q];
     }
-    out[q] = dw;
-    out[a.C + q] = db;
-    const float w = a.w ? a.w[wk.base + q] : 1.0f;
-    dws[q] = dw * w;
-    dbs[q] = db * w;
+    dw = team_sum(dw, per);
+    db = team_sum(db, per);
+    if (l == 0) {   // row 0 of a channel is this team's own
+      out[q] = dw;
+      out[a.C + q] = db;
+      const float w = a.w ? a.w[wk.base + q] : 1.0f;
+      dws[q] = dw * w;
+      dbs[q] = db * w;
+    }
   }
   __syncthreads();
   const int lanes = lanes_for(min(a.Cg, wk.local));
@@ -650,22 +670,17 @@ __global__ __launch_bounds__(256) void k_norm_grad_apply(NormArgs a) {
   });
 }
 
-// dweight and dbias: the fixed-order sum of the partial rows [part_rows][2][S][C] (row r of S C: q = r / S, at q 2 S + r - q S = q S + r; S = 1 but in the rows
-// form of one group over several positions); 16 channels x 64 row lanes per workgroup.
-__global__ __launch_bounds__(1024) void k_norm_param_sum(NormArgs a, int S) {
+// dweight and dbias: the fixed-order sum of the partial rows [part_rows][2][C]; 16 channels x 64 row lanes per workgroup.
+__global__ __launch_bounds__(1024) void k_norm_param_sum(NormArgs a) {
   __shared__ float sh[64][17];
   const int col = threadIdx.x & 15, lane = threadIdx.x >> 4, c = blockIdx.x * 16 + col;
   float* out = blockIdx.y ? a.db : a.dw;
   if (!out) return;
   float s = 0.0f;
   if (c < a.C) {
-    const float* p = a.part + blockIdx.y * (int64_t)S * a.C + c;
-    const int64_t rows = (int64_t)a.part_rows * S;
+    const float* p = a.part + (int64_t)blockIdx.y * a.C + c;
 #pragma unroll 8
-    for (int64_t r = lane; r < rows; r += 64) {
-      const int64_t q = S == 1 ? r : r / S;
-      s += p[(q * S + r) * a.C];
-    }
+    for (int r = lane; r < a.part_rows; r += 64) s += p[(int64_t)r * 2 * a.C];
   }
   sh[lane][col] = s;
   __syncthreads();
@@ -678,6 +693,8 @@ __global__ __launch_bounds__(1024) void k_norm_param_sum(NormArgs a, int S) {
 
 // -------------------------------------------------------------------- host side -------
 
+// Workgroups per CU, each for many rows: 262144 x 256 bf16 with SiLU, forward 8 per CU 52 us, 2 60, 32 70; backward 3 per CU 85
+// (with dropout 112), 2 80 (121), 8 92 (110).
 static bool plan_rows(const auv_norm* d, bool dense, bool backward, NormPlan& p) {
   const int full = d->type == AUV_BF16 ? 8 : 4;
   const int64_t m = (int64_t)d->s * (d->c / d->groups);
@@ -692,16 +709,17 @@ static bool plan_rows(const auv_norm* d, bool dense, bool backward, NormPlan& p)
   while (p.R * p.lanes < vecs) p.R *= 2;
   const int per = 256 / p.lanes, unit = d->groups / std::gcd(d->groups, per);   // teams: a multiple of the groups
   const int64_t rows = (int64_t)d->n * d->groups;
-  const int64_t most = (int64_t)compute_units() * (backward ? 4 : 8);
+  const int64_t most = (int64_t)compute_units() * (backward ? 3 : 8);   // workgroups, see below
   if (unit > most) return false;
   const int64_t want = std::min((rows - 1) / per + 1, most);
   p.blocks = (int)(want < unit ? unit : want / unit * unit);
-  p.part_rows = d->groups == 1 ? p.blocks : (int64_t)p.blocks * per / d->groups;
-  p.width = d->groups == 1 ? p.m : d->c;
+  p.part_rows = d->groups <= per ? p.blocks : (int64_t)p.blocks * per / d->groups;
   return true;
 }
 
-// Up to four vectors per thread of at most 512; several samples per workgroup where one leaves threads idle.
+// Up to four vectors per thread of at most 512; several samples per workgroup where one leaves threads idle.  Workgroups per CU,
+// each for many samples, keep weights and sums: 262144 x 8 x 3 bf16 in 3 groups, forward 6 per CU 44 us, 4 60, 16 47;
+// backward 4 per CU 67, 6 52, and 30000 x 8 x 32 in 8 groups 44 and 49.
 static bool plan_block(const auv_norm* d, bool backward, NormPlan& p) {
   const int full = d->type == AUV_BF16 ? 8 : 4;
   p.form = NORM_BLOCK;
@@ -723,13 +741,13 @@ static bool plan_block(const auv_norm* d, bool backward, NormPlan& p) {
     p.R = need > 2 ? 4 : need;
   }
   const int64_t want = (d->n - 1) / p.pack + 1;
-  p.blocks = (int)std::min<int64_t>(want, (int64_t)compute_units() * (backward ? 4 : 16));
+  p.blocks = (int)std::min<int64_t>(want, (int64_t)compute_units() * (backward ? 4 : 6));
   p.part_rows = p.blocks;
-  p.width = d->c;
   return true;
 }
 
-// Chunks of at least four passes of a workgroup, four workgroups per CU where the positions allow.
+// Chunks of at least four passes of a workgroup, two workgroups per CU where the positions allow (4 x 8192 x 512 bf16 in 32
+// groups, forward and backward: two per CU 31 and 50 us, four 39 and 61, one pass per chunk more still).
 static int plan_chunks(const char* fn, const auv_norm* d, NormPlan& p) {
   // a workgroup per sample at least, whose threads a launch counts in 32 bits
   if (d->n >= (1 << 24)) return set_error(AUV_EINVAL, "%s: n must be below 2^24 for samples of this size", fn);
@@ -740,12 +758,11 @@ static int plan_chunks(const char* fn, const auv_norm* d, NormPlan& p) {
   p.tile = std::min(vecs, 256);
   p.tiles = (vecs - 1) / p.tile + 1;
   const int step = 256 / p.tile;
-  const int64_t want = ((int64_t)4 * compute_units() - 1) / ((int64_t)d->n * p.tiles) + 1;
+  const int64_t want = ((int64_t)2 * compute_units() - 1) / ((int64_t)d->n * p.tiles) + 1;
   p.chunks = (int)std::max<int64_t>(1, std::min<int64_t>(want, (d->s - 1) / (4 * step) + 1));
   p.per = (d->s - 1) / p.chunks + 1;
   p.chunks = (d->s - 1) / p.per + 1;
   p.part_rows = (int64_t)d->n * p.chunks;
-  p.width = d->c;
   return AUV_OK;
 }
 
@@ -755,13 +772,13 @@ static int plan(const char* fn, const auv_norm* d, bool dense, bool backward, No
   return plan_chunks(fn, d, p);
 }
 
-static int64_t part_floats(const NormPlan& p, bool backward) {
-  return backward ? (p.part_rows * 2 * p.width + 3) / 4 * 4 : 0;
+static int64_t part_floats(const NormPlan& p, int64_t c, bool backward) {
+  return backward ? (p.part_rows * 2 * c + 3) / 4 * 4 : 0;
 }
 
 static int64_t plan_bytes(const auv_norm* d, const NormPlan& p, bool backward) {
   const int64_t shares = p.form == NORM_CHUNKS ? (int64_t)d->n * p.chunks * p.tiles * d->groups * 2 : 0;
-  return (part_floats(p, backward) + shares) * (int64_t)sizeof(float);
+  return (part_floats(p, d->c, backward) + shares) * (int64_t)sizeof(float);
 }
 
 static int check_norm(const char* fn, const auv_norm* d) {
@@ -905,27 +922,25 @@ int auv_norm_backward(const auv_norm* d, const auv_norm_grad* g, void* work, voi
   a.dw = g->dweight;
   a.db = g->dbias;
   a.part = p.form != NORM_CHUNKS && !params ? nullptr : static_cast<float*>(work);
-  int S = 1;   // positions within a partial row
   void* args[1] = {&a};
   hipStream_t s = (hipStream_t)stream;
   if (p.form == NORM_ROWS) {
-    const size_t lds = d->groups == 1 && params ? 4 * 2 * sizeof(float) * p.m : 0;
+    const int teams = 256 / p.lanes;
+    const size_t lds = d->groups <= teams && params ? (size_t)teams * 2 * p.m * sizeof(float) : 0;
     if (int rc = launch_norm_rows(fn, a, p, bf16, true, lds, s)) return rc;
-    if (d->groups == 1) S = d->s;
   } else if (p.form == NORM_BLOCK) {
     if (int rc = launch_kernel(fn, AUV_BLOCK_KERNEL(k_norm_block_grad), dim3(p.blocks), dim3(p.threads), args, block_lds(d, p), s))
       return rc;
   } else {
     const dim3 grid((unsigned)p.part_rows, p.tiles);
     const size_t lds = 2 * sizeof(float) * (256 / p.tile) * p.tile * p.V;
-    a.groups = a.part + part_floats(p, true);
+    a.groups = a.part + part_floats(p, d->c, true);
     if (int rc = launch_kernel(fn, AUV_CHUNK_KERNEL(k_norm_grad_sums), grid, dim3(256), args, lds, s)) return rc;
     if (int rc = launch_kernel(fn, AUV_CHUNK_KERNEL(k_norm_grad_apply), grid, dim3(256), args, 2 * sizeof(float) * tile_groups(d, p), s))
       return rc;
   }
   if (!params) return AUV_OK;
-  void* sum_args[2] = {&a, &S};
-  return launch_kernel(fn, (const void*)k_norm_param_sum, dim3((d->c - 1) / 16 + 1, 2), dim3(1024), sum_args, 0, s);
+  return launch_kernel(fn, (const void*)k_norm_param_sum, dim3((d->c - 1) / 16 + 1, 2), dim3(1024), args, 0, s);
 }
 
 }  // extern "C"

@@ -15,7 +15,7 @@ struct NormArgs {
   int64_t x_sn, x_ss, y_sn, y_ss, dout_sn, dout_ss, dx_sn, dx_ss;
   const float *w, *b;
   float *mean, *rstd;
-  float* part;    // backward: rows of partial sums of dw and db, [2][channels] each
+  float* part;    // backward: rows of partial sums of dw and db, [2][C] each
   float* groups;  // chunk form: [n][chunk][tile][G][2] moments (forward) or sums of d and d xhat (backward)
   float *dw, *db;
   float eps;
@@ -34,7 +34,7 @@ struct NormPlan {
   NormForm form;
   int V, R, blocks, threads;   // vector; vectors per lane (rows) or thread (block); workgroups of the launch and their size
   int m, lanes, tile, tiles, step, pack, chunks, per;
-  int64_t part_rows, width;    // backward: partial rows of [2][width] floats
+  int64_t part_rows;           // backward: partial rows of [2][C] floats
 };
 
 // Sum over a team of 1 to 64 lanes (a power of two), every lane gets it: moves within rows of 16

@@ -204,9 +204,9 @@ __global__ __launch_bounds__(256) void k_norm_rows_grad(NormArgs a) {
     }
   }
   if (!a.part) return;
-  // [part row][2][channels]: a team's own sums where there are several groups (team t holds group
-  // t mod G), else the workgroup's
-  if (a.G > 1) {
+  // [part row][2][C].  More groups than teams: a team's own sums, team t those of group t mod G; else the workgroup's,
+  // summed over its teams of a group (and over positions) through LDS.
+  if (a.G > per) {
     float* p = a.part + first * 2 * a.C + g * a.m;
 #pragma unroll
     for (int j = 0; j < NV; ++j)
@@ -218,31 +218,25 @@ __global__ __launch_bounds__(256) void k_norm_rows_grad(NormArgs a) {
         }
     return;
   }
-  extern __shared__ float red[];   // [waves][2][m]
+  extern __shared__ float red[];   // [teams][2][m]
+  float* own = red + tm.team * 2 * a.m;
 #pragma unroll
   for (int j = 0; j < NV; ++j)
 #pragma unroll
     for (int k = 0; k < V; ++k)
-      for (int s = a.lanes; s < 64; s <<= 1) {
-        dw[j][k] += __shfl_xor(dw[j][k], s);
-        db[j][k] += __shfl_xor(db[j][k], s);
+      if (k >= tm.shift[j]) {
+        own[tm.at[j] + k] = dw[j][k];
+        own[a.m + tm.at[j] + k] = db[j][k];
       }
-  const int wave = threadIdx.x >> 6;
-  if ((int)(threadIdx.x & 63) < a.lanes) {
-#pragma unroll
-    for (int j = 0; j < NV; ++j)
-#pragma unroll
-      for (int k = 0; k < V; ++k)
-        if (k >= tm.shift[j]) {
-          red[(2 * wave) * a.m + tm.at[j] + k] = dw[j][k];
-          red[(2 * wave + 1) * a.m + tm.at[j] + k] = db[j][k];
-        }
-  }
   __syncthreads();
-  for (int i = threadIdx.x; i < 2 * a.m; i += 256) {
+  const int g0 = (int)((int64_t)blockIdx.x * per % a.G);   // the first team's group
+  for (int i = threadIdx.x; i < 2 * a.C; i += 256) {
+    const int plane = i >= a.C, c = i - plane * a.C;
+    const int group = a.S == 1 ? c / a.m : 0, at = plane * a.m + (a.S == 1 ? c - group * a.m : c);
     float s = 0.0f;
-    for (int q = 0; q < 4; ++q) s += red[2 * q * a.m + i];
-    a.part[(int64_t)blockIdx.x * 2 * a.m + i] = s;
+    for (int t = (group - g0 + a.G) % a.G; t < per; t += a.G)
+      for (int pos = 0; pos < a.S; ++pos) s += red[t * 2 * a.m + at + pos * a.C];
+    a.part[(int64_t)blockIdx.x * 2 * a.C + i] = s;
   }
 }
 
