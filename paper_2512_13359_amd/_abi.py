@@ -204,10 +204,15 @@ def ptr(t) -> int | None:
 address = ctypes.addressof   # host address of a structure
 
 
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+
+
 def stream_ptr(stream=None) -> int | None:
-    import torch
-    s = torch.cuda.current_stream() if stream is None else stream
-    return s.cuda_stream or None
+    if stream is not None:
+        return stream.cuda_stream or None
+    if _raw_stream is not None:     # without the stream object (2.5 us of a call)
+        return _raw_stream(torch.cuda.current_device()) or None
+    return torch.cuda.current_stream().cuda_stream or None
 
 
 # ---- the C entry points, same names ---------------------------------------------------

@@ -73,6 +73,8 @@ template <int V> struct Draws {
         w[0] = j & 1u ? u >> 16 : u;
       }
     } else {
+      // kept from sharing the block above, which would then become bits first in either case
+      asm volatile("" : "+v"(row));
       uint32_t m = drop_bits(D, row, c >> 3) >> j;
       if (j + V > 8) m |= drop_bits(D, row, (c >> 3) + 1) << (8 - j);
       set(m);

@@ -37,24 +37,38 @@ struct NormPlan {
   int64_t part_rows;           // backward: partial rows of [2][C] floats
 };
 
-// Sum over a team of 1 to 64 lanes (a power of two), every lane gets it: moves within rows of 16
-// lanes, then lane swaps.
-__device__ __forceinline__ float team_sum(float v, int lanes) {
-  if (lanes > 1) v += dpp_move<DPP_QUAD_SWAP1>(v);
-  if (lanes > 2) v += dpp_move<DPP_QUAD_SWAP2>(v);
-  if (lanes > 4) v += dpp_move<DPP_ROW_HALF_MIRROR>(v);   // the other quad of eight lanes, equal in its four
-  if (lanes > 8) v += dpp_move<DPP_ROW_MIRROR>(v);
-  if (lanes > 16) {
+// Sum over a team of LANES lanes (a power of two), every lane gets it: moves within rows of 16 lanes, then lane swaps.
+template <int LANES> __device__ __forceinline__ float lanes_sum(float v) {
+  if constexpr (LANES > 1) v += dpp_move<DPP_QUAD_SWAP1>(v);
+  if constexpr (LANES > 2) v += dpp_move<DPP_QUAD_SWAP2>(v);
+  if constexpr (LANES > 4) v += dpp_move<DPP_ROW_HALF_MIRROR>(v);   // the other quad of eight lanes, equal in its four
+  if constexpr (LANES > 8) v += dpp_move<DPP_ROW_MIRROR>(v);
+  if constexpr (LANES > 16) {
     float u = v;
     asm("s_nop 1\n\tv_permlane16_swap_b32 %0, %1" : "+v"(v), "+v"(u));
     v += u;
   }
-  if (lanes > 32) {
+  if constexpr (LANES > 32) {
     float u = v;
     asm("s_nop 1\n\tv_permlane32_swap_b32 %0, %1" : "+v"(v), "+v"(u));
     v += u;
   }
   return v;
+}
+// the same for a number of lanes that the launch knows
+__device__ __forceinline__ float team_sum(float v, int lanes) {
+  if (lanes == 64) return lanes_sum<64>(v);
+  if (lanes == 32) return lanes_sum<32>(v);
+  if (lanes == 16) return lanes_sum<16>(v);
+  if (lanes == 8) return lanes_sum<8>(v);
+  if (lanes == 4) return lanes_sum<4>(v);
+  return lanes == 2 ? lanes_sum<2>(v) : v;
+}
+// two sums at once
+__device__ __forceinline__ void team_sums(float& v, float& u, int lanes) {
+  if (lanes == 64) v = lanes_sum<64>(v), u = lanes_sum<64>(u);
+  else if (lanes == 32) v = lanes_sum<32>(v), u = lanes_sum<32>(u);
+  else v = team_sum(v, lanes), u = team_sum(u, lanes);
 }
 
 int launch_norm_rows(const char* fn, const NormArgs& a, const NormPlan& p, bool bf16, bool grad, size_t lds, hipStream_t s);

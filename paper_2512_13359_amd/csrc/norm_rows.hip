@@ -189,8 +189,9 @@ __global__ __launch_bounds__(256) void k_norm_rows_grad(NormArgs a) {
         s1 += d[j][k];
         s2 = __builtin_fmaf(d[j][k], xh[j][k], s2);
       }
-    s1 = team_sum(s1, a.lanes) * inv;
-    s2 = team_sum(s2, a.lanes) * inv;
+    team_sums(s1, s2, a.lanes);
+    s1 *= inv;
+    s2 *= inv;
     const float f = rstd * a.drop.scale;
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
