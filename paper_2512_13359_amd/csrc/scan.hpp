@@ -202,9 +202,9 @@ int launch_scan_forward(const ScanArgs& a, const ScanShape& sh, bool bf16, bool 
 int launch_scan_backward(const ScanArgs& a, const ScanShape& sh, bool bf16, bool sig, hipStream_t s);
 
 // The instance of kernel family KERN for a shape: KERN<T, V, SIG, MASK, NI>
-#define AUV_SCAN_PICK(KERN, T, V, SIG)                                                            \
-  (mask ? (sh.ni ? (const void*)KERN<T, V, SIG, true, true> : (const void*)KERN<T, V, SIG, true, false>) \
-        : (const void*)KERN<T, V, SIG, false, false>)
+#define AUV_SCAN_AXIS(KERN, T, V, SIG, MASK) \
+  (sh.ni ? (const void*)KERN<T, V, SIG, MASK, true> : (const void*)KERN<T, V, SIG, MASK, false>)
+#define AUV_SCAN_PICK(KERN, T, V, SIG) (mask ? AUV_SCAN_AXIS(KERN, T, V, SIG, true) : AUV_SCAN_AXIS(KERN, T, V, SIG, false))
 #define AUV_SCAN_KIND(KERN, T, V) (sig ? AUV_SCAN_PICK(KERN, T, V, true) : AUV_SCAN_PICK(KERN, T, V, false))
 #define AUV_SCAN_KERNEL(KERN)                        \
   (bf16 ? (sh.V == 4   ? AUV_SCAN_KIND(KERN, __bf16, 4) \

@@ -50,6 +50,7 @@ def seq(g, T, n, c, typ, order, scale=1.0, shift=0.0):
 
 
 def scan_inputs(T, n, c, typ, kind, order, masks, seed=0):
+    """masks: d episode ends, l lengths (in "plain" too, which has no initial state), h an initial state only, "" nothing."""
     g = torch.Generator(device="cuda")
     g.manual_seed(seed)
     if order == "ntc2":     # gate and input as the halves of one buffer
@@ -60,7 +61,7 @@ def scan_inputs(T, n, c, typ, kind, order, masks, seed=0):
     if kind == "decay":
         gate.copy_(torch.sigmoid(gate.float()) * 1.25 - 0.3)     # negative, zero-crossing and above one too
     done = lens = None
-    h0 = torch.randn((n, c), generator=g, device="cuda") if masks != "plain" else None
+    h0 = torch.randn((n, c), generator=g, device="cuda") if masks not in ("", "plain") else None
     if "d" in masks:
         done = (torch.rand((T, n), generator=g, device="cuda") < 0.07).float()
         done[:, 0] = 1.0                                         # a sequence that ends at every step
@@ -110,6 +111,18 @@ def test_scan_orders(order, typ):
     for T, n, c, masks in ((37, 6, 9, "dl"), (37, 9, 6, "plain"), (64, 67, 40, "d"), (3, 1, 13, "l"), (1200, 3, 4, "dl"), (9, 130, 1, "dl")):
         announce(f"scan order {order} T={T} n={n} c={c} {typ} {masks}")
         check_scan(T, n, c, typ, "sigmoid", order, masks, seed=c)
+
+
+@pytest.mark.parametrize("order", ["tnc", "ntc2", "cnt", "nct", "tcn"])
+@pytest.mark.parametrize("kind", ["sigmoid", "decay"])
+def test_scan_orders_without_masks(order, kind):
+    """No episode ends, no lengths, with and without an initial state, the sequence or the channel as the longer axis."""
+    require_gpu()
+    for T, n, c in ((20, 50, 6), (20, 6, 50), (1, 9, 40), (1300, 2, 9), (5, 700, 31)):
+        for masks in ("", "h"):
+            for typ in ("fp32", "bf16"):
+                announce(f"scan order {order} T={T} n={n} c={c} {typ} {kind} masks '{masks}'")
+                check_scan(T, n, c, typ, kind, order, masks, seed=n)
 
 
 @pytest.mark.parametrize("typ", ["fp32", "bf16"])
@@ -162,6 +175,21 @@ def test_scan_masked_places_hold_anything(T, typ):
     for p, q in zip(a, d):
         assert torch.equal(p[:5], q[:5])
     assert torch.isnan(d[1][5:8, 0]).all() and torch.equal(d[1][:, 1:], a[1][:, 1:])
+
+
+@pytest.mark.parametrize("seed", range(6))
+def test_scan_drawn(seed):
+    """Sizes, orders, kinds, types and masks drawn together."""
+    require_gpu()
+    r = np.random.default_rng(seed)
+    log = lambda lo, hi: int(round(np.exp(r.uniform(np.log(lo), np.log(hi)))))  # noqa: E731
+    for _ in range(12):
+        T, c = log(1, 3000), log(1, 300)
+        n = log(1, max(1, min(3000, 600000 // (T * c))))
+        typ, kind = str(r.choice(["fp32", "bf16"])), str(r.choice(["sigmoid", "decay"]))
+        order, masks = str(r.choice(["tnc", "ntc", "ntc2", "cnt", "nct", "tcn", "odd"])), str(r.choice(["", "h", "d", "l", "dl"]))
+        announce(f"scan T={T} n={n} c={c} {typ} {kind} {order} masks '{masks}'")
+        check_scan(T, n, c, typ, kind, order, masks, seed=seed)
 
 
 def test_scan_extreme_gates():
@@ -313,6 +341,23 @@ def test_norm_groups(n, s, c, groups, typ):
     announce(f"norm groups n={n} s={s} c={c} g={groups} {typ}")
     check_norm(n, s, c, groups, typ, "silu", seed=c)
     check_norm(n, s, c, groups, typ, "none", drop=20000, pitch=3, affine=False, seed=c)
+
+
+@pytest.mark.parametrize("seed", range(6))
+def test_norm_drawn(seed):
+    """Sizes, groups, types, activations, dropout and pitches drawn together, all three forms."""
+    require_gpu()
+    r = np.random.default_rng(100 + seed)
+    log = lambda lo, hi: int(round(np.exp(r.uniform(np.log(lo), np.log(hi)))))  # noqa: E731
+    for _ in range(12):
+        groups = int(r.choice([1, 1, 2, 3, 8, 32]))
+        c = groups * log(1, 3000 // groups)
+        s = 1 if r.random() < 0.4 else log(2, 4000)
+        n = log(1, max(1, min(3000, 600000 // (s * c))))
+        typ, act = str(r.choice(["fp32", "bf16"])), str(r.choice(["none", "relu", "silu", "tanh"]))
+        drop, pitch, affine = int(r.choice([0, 655, 20000])), int(r.choice([0, 0, 1, 8])), bool(r.random() < 0.8)
+        announce(f"norm n={n} s={s} c={c} g={groups} {typ} {act} drop={drop} pitch={pitch} affine={affine}")
+        check_norm(n, s, c, groups, typ, act, drop, pitch, affine, seed=seed)
 
 
 @pytest.mark.parametrize("s, c, groups", [(1, 256, 1), (500, 16, 2)])
