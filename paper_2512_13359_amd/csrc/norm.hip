@@ -303,9 +303,9 @@ __global__ __launch_bounds__(512) void k_norm_block_grad(NormArgs a) {
   for (int plane = 0; plane < 2; ++plane) {
     column_sums<V>(a, tm, plane ? db : dw, false, rows, parts, cols);
     for (int c = threadIdx.x; c < a.C; c += blockDim.x) {
-      float s = 0.0f;
-      for (int p = 0; p < a.pack; ++p) s += cols[p * a.C + c];
-      a.part[((int64_t)blockIdx.x * 2 + plane) * a.C + c] = s;
+      double s = 0.0;
+      for (int p = 0; p < a.pack; ++p) s += (double)cols[p * a.C + c];
+      a.part[((int64_t)blockIdx.x * 2 + plane) * a.C + c] = (float)s;
     }
     __syncthreads();
   }
@@ -670,17 +670,18 @@ __global__ __launch_bounds__(256) void k_norm_grad_apply(NormArgs a) {
   });
 }
 
-// dweight and dbias: the fixed-order sum of the partial rows [part_rows][2][C]; 16 channels x 64 row lanes per workgroup.
+// dweight and dbias: the fixed-order sum of the partial rows [part_rows][2][C], in 64 bits (a chain of additions in 32 would
+// cost the sums of many rows a digit); 16 channels x 64 row lanes per workgroup.
 __global__ __launch_bounds__(1024) void k_norm_param_sum(NormArgs a) {
-  __shared__ float sh[64][17];
+  __shared__ double sh[64][17];
   const int col = threadIdx.x & 15, lane = threadIdx.x >> 4, c = blockIdx.x * 16 + col;
   float* out = blockIdx.y ? a.db : a.dw;
   if (!out) return;
-  float s = 0.0f;
+  double s = 0.0;
   if (c < a.C) {
     const float* p = a.part + (int64_t)blockIdx.y * a.C + c;
 #pragma unroll 8
-    for (int r = lane; r < a.part_rows; r += 64) s += p[(int64_t)r * 2 * a.C];
+    for (int r = lane; r < a.part_rows; r += 64) s += (double)p[(int64_t)r * 2 * a.C];
   }
   sh[lane][col] = s;
   __syncthreads();
@@ -688,7 +689,7 @@ __global__ __launch_bounds__(1024) void k_norm_param_sum(NormArgs a) {
     if (lane < d) sh[lane][col] += sh[lane + d][col];
     __syncthreads();
   }
-  if (lane == 0 && c < a.C) out[c] = sh[0][col];
+  if (lane == 0 && c < a.C) out[c] = (float)sh[0][col];
 }
 
 // -------------------------------------------------------------------- host side -------

@@ -234,10 +234,10 @@ __global__ __launch_bounds__(256) void k_norm_rows_grad(NormArgs a) {
   for (int i = threadIdx.x; i < 2 * a.C; i += 256) {
     const int plane = i >= a.C, c = i - plane * a.C;
     const int group = a.S == 1 ? c / a.m : 0, at = plane * a.m + (a.S == 1 ? c - group * a.m : c);
-    float s = 0.0f;
+    double s = 0.0;
     for (int t = (group - g0 + a.G) % a.G; t < per; t += a.G)
-      for (int pos = 0; pos < a.S; ++pos) s += red[t * 2 * a.m + at + pos * a.C];
-    a.part[(int64_t)blockIdx.x * 2 * a.C + i] = s;
+      for (int pos = 0; pos < a.S; ++pos) s += (double)red[t * 2 * a.m + at + pos * a.C];
+    a.part[(int64_t)blockIdx.x * 2 * a.C + i] = (float)s;
   }
 }
 
