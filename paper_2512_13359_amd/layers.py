@@ -8,6 +8,8 @@ into a graph.  The functions are not part of torch's autograd: gradients come fr
 functions.  Wrong arguments raise AuvError before anything is enqueued."""
 from __future__ import annotations
 
+import struct
+
 import torch
 
 from . import _abi as A
@@ -16,6 +18,11 @@ TYPES = {torch.float32: A.AUV_FP32, torch.bfloat16: A.AUV_BF16}
 KINDS = {"sigmoid": A.AUV_SCAN_SIGMOID, "decay": A.AUV_SCAN_DECAY}
 ACTS = {"none": A.AUV_ACTIVATION_NONE, "relu": A.AUV_ACTIVATION_RELU, "silu": A.AUV_ACTIVATION_SILU,
         "tanh": A.AUV_ACTIVATION_TANH}
+
+# The larger structures packed at once, in half the time of setting their fields one by one; _NONE
+# stands for a tensor that is not given.
+_SCAN, _SCAN_GRAD, _NORM = struct.Struct("@5i4x4q4q4q2q3q3q"), struct.Struct("@4q3q4q4q3q"), struct.Struct("@6if4x3q5q")
+_NONE = (0, 0, 0)
 
 
 def _refuse(fn: str, msg: str):
@@ -29,64 +36,73 @@ def _one_of(fn, what, choices, v):
 
 
 def _like(fn, name, t, shape, dtype, device, contiguous=False):
-    """Checks an optional tensor; returns it."""
-    if t is None:
-        return None
-    if t.dtype != dtype or tuple(t.shape) != shape:
+    """Checks a tensor."""
+    if t.dtype != dtype or t.shape != shape:
         _refuse(fn, f"{name} must be {dtype} of shape {tuple(shape)}, got {t.dtype} of {tuple(t.shape)}")
     if t.device != device:
         _refuse(fn, f"{name} is on {t.device}, x on {device}")
     if contiguous and not t.is_contiguous():
         _refuse(fn, f"{name} must be contiguous")
-    return t
 
 
 def _here(fn, x, stream) -> bool:
     """Whether x's device is the current one and the stream its current stream."""
     if not x.is_cuda:
         _refuse(fn, f"tensors must be on a GPU, x is on {x.device}")
-    return stream is None and x.device.index == torch.cuda.current_device()
+    return stream is None and x.get_device() == torch.cuda.current_device()
 
 
-def _moved(x, stream):
+def _packed(fn, kind, layout, *words):
+    try:
+        return kind.from_buffer_copy(layout.pack(*words))
+    except (struct.error, OverflowError) as e:
+        _refuse(fn, f"a size, stride or number is out of range: {e}")
+
+
+class _Moved:
     """Makes x's device and the stream current: the call inside allocates and launches there."""
-    class Scope:
-        def __enter__(self):
-            self.d = torch.cuda.device(x.device)
-            self.d.__enter__()
-            self.s = torch.cuda.stream(stream)
-            self.s.__enter__()
 
-        def __exit__(self, *e):
-            self.s.__exit__(*e)
-            self.d.__exit__(*e)
-    return Scope()
+    def __init__(self, x, stream):
+        self.scopes = (torch.cuda.device(x.device), torch.cuda.stream(stream))
+
+    def __enter__(self):
+        for s in self.scopes:
+            s.__enter__()
+
+    def __exit__(self, *e):
+        for s in reversed(self.scopes):
+            s.__exit__(*e)
 
 
-def _empty(n: int, x) -> torch.Tensor | None:
+def _work(n: int, x) -> torch.Tensor | None:
     return torch.empty(n, dtype=torch.uint8, device=x.device) if n else None
 
 
 # ---- gated linear recurrence ---------------------------------------------------------
 
 def _scan(fn, gate, x, kind, done, lens, h0):
-    if x.dim() != 3 or x.dtype not in TYPES:
-        _refuse(fn, f"x must be a float32 or bfloat16 tensor [T][n][c], got {x.dtype} of {tuple(x.shape)}")
-    T, n, c = x.shape
-    dev = x.device
-    _like(fn, "gate", gate, x.shape, x.dtype, dev)
-    _like(fn, "done", done, (T, n), torch.float32, dev, True)
-    _like(fn, "lens", lens, (n,), torch.int32, dev, True)
-    _like(fn, "h0", h0, (n, c), torch.float32, dev)
-    return T, n, c
+    """The structure's first words and its inputs' addresses and strides."""
+    shape, dtype, dev = x.shape, x.dtype, x.device
+    if len(shape) != 3 or dtype not in TYPES:
+        _refuse(fn, f"x must be a float32 or bfloat16 tensor [T][n][c], got {dtype} of {tuple(shape)}")
+    T, n, c = shape
+    _like(fn, "gate", gate, shape, dtype, dev)
+    if done is not None:
+        _like(fn, "done", done, (T, n), torch.float32, dev, True)
+    if lens is not None:
+        _like(fn, "lens", lens, (n,), torch.int32, dev, True)
+    if h0 is not None:
+        _like(fn, "h0", h0, (n, c), torch.float32, dev)
+    return (T, n, c, TYPES[dtype], _one_of(fn, "kind", KINDS, kind), gate.data_ptr(), *gate.stride(), x.data_ptr(), *x.stride())
 
 
-def _seq(t):
-    return (0, 0, 0, 0) if t is None else (t.data_ptr(), *t.stride())
+def _at(t):
+    """Address and strides of a tensor, of a state that may be absent."""
+    return _NONE if t is None else (t.data_ptr(), *t.stride())
 
 
-def _state(t):
-    return (0, 0, 0) if t is None else (t.data_ptr(), *t.stride())
+def _masks(done, lens, h0):
+    return (0 if done is None else done.data_ptr(), 0 if lens is None else lens.data_ptr(), *_at(h0))
 
 
 def scan_forward(gate, x, *, kind="sigmoid", done=None, lens=None, h0=None, out=None, stream=None):
@@ -100,17 +116,16 @@ def scan_forward(gate, x, *, kind="sigmoid", done=None, lens=None, h0=None, out=
     h has x's type and memory order, or is `out`; last = s_{T-1} and h0 are float32 [n][c].  One step
     (T = 1) is the form for a controller: pass `last` back as the next h0."""
     fn = "scan_forward"
-    T, n, c = _scan(fn, gate, x, kind, done, lens, h0)
-    k = _one_of(fn, "kind", KINDS, kind)
-    _like(fn, "out", out, x.shape, x.dtype, x.device)
+    head = _scan(fn, gate, x, kind, done, lens, h0)
+    if out is not None:
+        _like(fn, "out", out, x.shape, x.dtype, x.device)
     if not _here(fn, x, stream):
-        with _moved(x, stream):
+        with _Moved(x, stream):
             return scan_forward(gate, x, kind=kind, done=done, lens=lens, h0=h0, out=out)
     h = torch.empty_like(x) if out is None else out
-    last = torch.empty((n, c), dtype=torch.float32, device=x.device) if h0 is None else torch.empty_like(h0)
-    d = A.AuvScan(T, n, c, TYPES[x.dtype], k, *_seq(gate), *_seq(x), *_seq(h), A.ptr(done), A.ptr(lens), *_state(h0),
-                  *_state(last))
-    A.auv_scan_forward(d, _empty(A.auv_scan_work_bytes(d), x))
+    last = torch.empty(x.shape[1:], dtype=torch.float32, device=x.device) if h0 is None else torch.empty_like(h0)
+    d = _packed(fn, A.AuvScan, _SCAN, *head, *_at(h), *_masks(done, lens, h0), *_at(last))
+    A.auv_scan_forward(d, _work(A.auv_scan_work_bytes(d), x))
     return h, last
 
 
@@ -121,35 +136,38 @@ def scan_backward(gate, x, h, *, dout=None, dh_last=None, kind="sigmoid", done=N
     dgate and dx have x's type (zero at held steps), or are the pair `out`: the halves of one
     buffer, say, where gate and x are the halves of one projection.  dh0 is float32 [n][c]."""
     fn = "scan_backward"
-    T, n, c = _scan(fn, gate, x, kind, done, lens, h0)
-    k = _one_of(fn, "kind", KINDS, kind)
+    head = _scan(fn, gate, x, kind, done, lens, h0)
     _like(fn, "h", h, x.shape, x.dtype, x.device)
-    _like(fn, "dout", dout, x.shape, x.dtype, x.device)
-    _like(fn, "dh_last", dh_last, (n, c), torch.float32, x.device)
+    if dout is not None:
+        _like(fn, "dout", dout, x.shape, x.dtype, x.device)
+    if dh_last is not None:
+        _like(fn, "dh_last", dh_last, x.shape[1:], torch.float32, x.device)
     for o in out or ():
         _like(fn, "out", o, x.shape, x.dtype, x.device)
     if not _here(fn, x, stream):
-        with _moved(x, stream):
+        with _Moved(x, stream):
             return scan_backward(gate, x, h, dout=dout, dh_last=dh_last, kind=kind, done=done, lens=lens, h0=h0, out=out)
     dgate, dx = (torch.empty_like(gate), torch.empty_like(x)) if out is None else out
     like = h0 if h0 is not None else dh_last
-    dh0 = torch.empty((n, c), dtype=torch.float32, device=x.device) if like is None else torch.empty_like(like)
-    d = A.AuvScan(T, n, c, TYPES[x.dtype], k, *_seq(gate), *_seq(x), *_seq(h), A.ptr(done), A.ptr(lens), *_state(h0))
-    g = A.AuvScanGrad(*_seq(dout), *_state(dh_last), *_seq(dgate), *_seq(dx), *_state(dh0))
-    A.auv_scan_backward(d, g, _empty(A.auv_scan_work_bytes(d, g), x))
+    dh0 = torch.empty(x.shape[1:], dtype=torch.float32, device=x.device) if like is None else torch.empty_like(like)
+    d = _packed(fn, A.AuvScan, _SCAN, *head, *_at(h), *_masks(done, lens, h0), *_NONE)
+    g = _packed(fn, A.AuvScanGrad, _SCAN_GRAD, *(_at(dout) if dout is not None else (0, 0, 0, 0)), *_at(dh_last), *_at(dgate),
+                *_at(dx), *_at(dh0))
+    A.auv_scan_backward(d, g, _work(A.auv_scan_work_bytes(d, g), x))
     return dgate, dx, dh0
 
 
 # ---- group norm and dropout ----------------------------------------------------------
 
-def _rows(fn, name, t):
+def _sizes(fn, x):
     """(n, s, c) of a channels-last tensor [n][c] or [n][s][c]."""
-    if t.dim() not in (2, 3) or t.dtype not in TYPES:
-        _refuse(fn, f"{name} must be a float32 or bfloat16 tensor [n][c] or [n][s][c], got {t.dtype} of {tuple(t.shape)}")
-    return (t.shape[0], 1, t.shape[1]) if t.dim() == 2 else tuple(t.shape)
+    shape = x.shape
+    if len(shape) not in (2, 3) or x.dtype not in TYPES:
+        _refuse(fn, f"x must be a float32 or bfloat16 tensor [n][c] or [n][s][c], got {x.dtype} of {tuple(shape)}")
+    return (shape[0], 1, shape[1]) if len(shape) == 2 else shape
 
 
-def _at(fn, name, t):
+def _rows(fn, name, t):
     """Address and strides (sample, position) of a channels-last tensor."""
     st = t.stride()
     if st[-1] != 1 and t.shape[-1] != 1:
@@ -167,25 +185,30 @@ def dropout(x, drop, add=None, *, out=None, stream=None):
     No mask is stored: the gradient is dropout of the gradient with the same `drop`.  `out` may be x or
     add itself."""
     fn = "dropout"
-    n, s, c = _rows(fn, "x", x)
-    _like(fn, "add", add, x.shape, x.dtype, x.device)
-    _like(fn, "out", out, x.shape, x.dtype, x.device)
+    n, s, c = _sizes(fn, x)
+    if add is not None:
+        _like(fn, "add", add, x.shape, x.dtype, x.device)
+    if out is not None:
+        _like(fn, "out", out, x.shape, x.dtype, x.device)
     if not _here(fn, x, stream):
-        with _moved(x, stream):
+        with _Moved(x, stream):
             return dropout(x, drop, add, out=out)
     y = _fresh(x) if out is None else out
-    A.auv_dropout(drop, TYPES[x.dtype], n, s, c, A.AuvRows(*_at(fn, "x", x)),
-                  None if add is None else A.AuvRows(*_at(fn, "add", add)), A.AuvRows(*_at(fn, "out", y)))
+    A.auv_dropout(drop, TYPES[x.dtype], n, s, c, A.AuvRows(*_rows(fn, "x", x)),
+                  None if add is None else A.AuvRows(*_rows(fn, "add", add)), A.AuvRows(*_rows(fn, "out", y)))
     return y
 
 
-def _norm(fn, x, groups, weight, bias, eps, act, drop, mean, rstd):
-    n, s, c = _rows(fn, "x", x)
-    _like(fn, "weight", weight, (c,), torch.float32, x.device, True)
-    _like(fn, "bias", bias, (c,), torch.float32, x.device, True)
-    # the callers hold `drop` while the structure is in use
-    return A.AuvNorm(n, s, c, groups, TYPES[x.dtype], _one_of(fn, "act", ACTS, act), eps, *_at(fn, "x", x), A.ptr(weight),
-                     A.ptr(bias), A.ptr(mean), A.ptr(rstd), None if drop is None else A.address(drop))
+def _norm(fn, x, groups, weight, bias, eps, act, drop):
+    """The structure without mean and rstd; the callers hold `drop` while it is in use."""
+    n, s, c = _sizes(fn, x)
+    if weight is not None:
+        _like(fn, "weight", weight, (c,), torch.float32, x.device, True)
+    if bias is not None:
+        _like(fn, "bias", bias, (c,), torch.float32, x.device, True)
+    return _packed(fn, A.AuvNorm, _NORM, n, s, c, groups, TYPES[x.dtype], _one_of(fn, "act", ACTS, act), eps, *_rows(fn, "x", x),
+                   0 if weight is None else weight.data_ptr(), 0 if bias is None else bias.data_ptr(), 0, 0,
+                   0 if drop is None else A.address(drop))
 
 
 def norm_forward(x, groups, *, weight=None, bias=None, eps=1e-5, act="none", drop=None, out=None, stream=None):
@@ -197,17 +220,18 @@ def norm_forward(x, groups, *, weight=None, bias=None, eps=1e-5, act="none", dro
     "silu", "tanh".  With `drop` (make_drop) x is dropped out first, its mask never stored.  mean and
     rstd are float32 [n][groups]; y has x's type, or is `out`."""
     fn = "norm_forward"
-    d = _norm(fn, x, groups, weight, bias, eps, act, drop, None, None)
-    _like(fn, "out", out, x.shape, x.dtype, x.device)
+    d = _norm(fn, x, groups, weight, bias, eps, act, drop)
+    if out is not None:
+        _like(fn, "out", out, x.shape, x.dtype, x.device)
     if not _here(fn, x, stream):
-        with _moved(x, stream):
+        with _Moved(x, stream):
             return norm_forward(x, groups, weight=weight, bias=bias, eps=eps, act=act, drop=drop, out=out)
-    work = _empty(A.auv_norm_work_bytes(d, False), x)
+    work = _work(A.auv_norm_work_bytes(d, False), x)
     y = _fresh(x) if out is None else out
     mean = torch.empty((d.n, groups), dtype=torch.float32, device=x.device)
     rstd = torch.empty_like(mean)
     d.mean, d.rstd = mean.data_ptr(), rstd.data_ptr()
-    A.auv_norm_forward(d, A.AuvRows(*_at(fn, "out", y)), work)
+    A.auv_norm_forward(d, A.AuvRows(*_rows(fn, "out", y)), work)
     return y, mean, rstd
 
 
@@ -216,17 +240,19 @@ def norm_backward(x, groups, mean, rstd, dout, *, weight=None, bias=None, act="n
     other arguments its own.  dx has x's type, or is `out`; dweight is None where weight is, dbias
     where bias is, else float32 [c]."""
     fn = "norm_backward"
-    d = _norm(fn, x, groups, weight, bias, 0.0, act, drop, mean, rstd)
+    d = _norm(fn, x, groups, weight, bias, 0.0, act, drop)
     for name, t in (("mean", mean), ("rstd", rstd)):
         _like(fn, name, t, (d.n, groups), torch.float32, x.device, True)
+    d.mean, d.rstd = mean.data_ptr(), rstd.data_ptr()
     _like(fn, "dout", dout, x.shape, x.dtype, x.device)
-    _like(fn, "out", out, x.shape, x.dtype, x.device)
+    if out is not None:
+        _like(fn, "out", out, x.shape, x.dtype, x.device)
     if not _here(fn, x, stream):
-        with _moved(x, stream):
+        with _Moved(x, stream):
             return norm_backward(x, groups, mean, rstd, dout, weight=weight, bias=bias, act=act, drop=drop, out=out)
-    work = _empty(A.auv_norm_work_bytes(d, True), x)
+    work = _work(A.auv_norm_work_bytes(d, True), x)
     dx = _fresh(x) if out is None else out
     dweight = None if weight is None else torch.empty_like(weight)
     dbias = None if bias is None else torch.empty_like(bias)
-    A.auv_norm_backward(d, A.AuvNormGrad(*_at(fn, "dout", dout), *_at(fn, "out", dx), A.ptr(dweight), A.ptr(dbias)), work)
+    A.auv_norm_backward(d, A.AuvNormGrad(*_rows(fn, "dout", dout), *_rows(fn, "out", dx), A.ptr(dweight), A.ptr(dbias)), work)
     return dx, dweight, dbias

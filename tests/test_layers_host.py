@@ -135,7 +135,49 @@ def test_functions_refuse():
            lambda: M.norm_forward(x, 1, weight=torch.zeros(7)), lambda: M.norm_forward(x, 1, act="gelu"),
            lambda: M.norm_forward(x.permute(0, 2, 1), 1), lambda: M.norm_backward(x, 2, torch.zeros(4, 1), torch.zeros(4, 2), x),
            lambda: M.norm_backward(x, 2, torch.zeros(4, 2), torch.zeros(4, 2), x[:, :1]),
+           lambda: M.norm_forward(x, 1 << 40), lambda: M.norm_forward(x, 1.5), lambda: M.norm_forward(x, 1, eps=1e300),
            lambda: M.dropout(x, M.make_drop(0.1, 1)), lambda: M.dropout(x, M.make_drop(0.1, 1), x.bfloat16())]
     for f in bad:
         with pytest.raises(M.AuvError):
             f()
+
+
+def test_packed_structures_are_the_bindings_own():
+    """The words that the functions pack land in the fields they are meant for, and the fields where a C++
+    compiler puts the header's."""
+    from paper_2512_13359_amd import _abi as A
+    from paper_2512_13359_amd import layers as L
+    for kind, layout in ((A.AuvScan, L._SCAN), (A.AuvScanGrad, L._SCAN_GRAD), (A.AuvNorm, L._NORM)):
+        names = [f[0] for f in kind._fields_]
+        got = kind.from_buffer_copy(layout.pack(*range(1, len(names) + 1)))
+        assert ctypes.sizeof(kind) == layout.size and [getattr(got, k) for k in names] == list(range(1, len(names) + 1))
+
+
+def test_structures_match_the_header(tmp_path):
+    """Sizes and offsets of the layers' structures, asked of a C++ compiler."""
+    import os
+    import shutil
+    import subprocess
+    from paper_2512_13359_amd import _abi as A
+    cxx = shutil.which("g++") or shutil.which("c++")
+    if cxx is None:
+        pytest.skip("needs a C++ compiler")
+    want = {"auv_scan": (A.AuvScan, {"gate_st": "gate.st", "x": "x.p", "h_sc": "h.sc", "done": "done", "h0": "h0.p", "last_sc": "last.sc"}),
+            "auv_scan_grad": (A.AuvScanGrad, {"dlast": "dlast.p", "dgate": "dgate.p", "dx_sn": "dx.sn", "dh0_sc": "dh0.sc"}),
+            "auv_drop": (A.AuvDrop, {"step": "step", "drop": "drop"}), "auv_rows": (A.AuvRows, {"ss": "ss"}),
+            "auv_norm": (A.AuvNorm, {"eps": "eps", "x_ss": "x.ss", "weight": "weight", "drop": "drop"}),
+            "auv_norm_grad": (A.AuvNormGrad, {"dx": "dx.p", "dweight": "dweight"})}
+    lines, expect = [], []
+    for name, (kind, fields) in want.items():
+        lines.append(f"sizeof({name})")
+        expect.append(ctypes.sizeof(kind))
+        for f, member in fields.items():
+            lines.append(f"offsetof({name}, {member})")
+            expect.append(getattr(kind, f).offset)
+    src = tmp_path / "a.cpp"
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    src.write_text('#include <cstddef>\n#include <cstdio>\n#include "auv.h"\nint main() {\n'
+                   + "".join(f'  std::printf("%zu\\n", (size_t){x});\n' for x in lines) + "}\n")
+    subprocess.run([cxx, "-std=c++17", f"-I{root}/include", str(src), "-o", str(tmp_path / "a")], check=True)
+    out = subprocess.run([str(tmp_path / "a")], check=True, capture_output=True, text=True).stdout
+    assert [int(x) for x in out.split()] == expect
