@@ -197,22 +197,24 @@ __global__ __launch_bounds__(512) void k_norm_block(NormArgs a) {
   }
 }
 
-template <class T, int V, int R, bool DROP>
+// Merged: the V channels of a thread are of one group, whose values are held once.
+template <class T, int V, int R, bool DROP, bool MERGED>
 __global__ __launch_bounds__(512) void k_norm_block_grad(NormArgs a) {
   extern __shared__ float lds[];
+  constexpr int VG = MERGED ? 1 : V;   // groups of a thread
   const BlockTeam<T, V, R> tm(a);
   const int width = a.pack * a.C, all = a.pack * a.G;
-  const bool merged = a.Cg % V == 0;   // a thread's channels are of one group
   float *m1 = lds, *m2 = m1 + all, *cols = m2 + all, *parts = cols + width, *rows = parts + blockDim.x;
   float w[V], b[V], dw[V], db[V];
-  int g[V];
+  int g[VG];
 #pragma unroll
   for (int k = 0; k < V; ++k) {
     w[k] = a.w ? a.w[tm.c + k] : 1.0f;
     b[k] = a.b ? a.b[tm.c + k] : 0.0f;
-    g[k] = tm.p * a.G + (tm.c + k) / a.Cg;
     dw[k] = db[k] = 0.0f;
   }
+#pragma unroll
+  for (int k = 0; k < VG; ++k) g[k] = tm.p * a.G + (tm.c + k) / a.Cg;
   const float inv = 1.0f / ((float)a.S * (float)a.Cg);
   for (int64_t first = (int64_t)blockIdx.x * a.pack; first < a.n; first += (int64_t)gridDim.x * a.pack) {
     const int64_t i = first + tm.p;
@@ -221,9 +223,9 @@ __global__ __launch_bounds__(512) void k_norm_block_grad(NormArgs a) {
     const T* dy = reinterpret_cast<const T*>(a.dout) + i * a.dout_sn + tm.c;
     Vec<T, V> q[R], e[R];
     Draws<V> keep[R];
-    float mean[V], rstd[V], s1[V], s2[V];
+    float mean[VG], rstd[VG], s1[V], s2[V];
 #pragma unroll
-    for (int k = 0; k < V; ++k) s1[k] = s2[k] = mean[k] = rstd[k] = 0.0f;
+    for (int k = 0; k < V; ++k) s1[k] = s2[k] = 0.0f;
 #pragma unroll
     for (int r = 0; r < R; ++r) {
       const int s = tm.row + r * a.step;
@@ -232,29 +234,28 @@ __global__ __launch_bounds__(512) void k_norm_block_grad(NormArgs a) {
         e[r].load(dy + s * a.dout_ss);
       }
     }
-    if (live) {
 #pragma unroll
-      for (int k = 0; k < V; ++k) {
-        mean[k] = a.mean[first * a.G + g[k]];
-        rstd[k] = a.rstd[first * a.G + g[k]];
-      }
+    for (int k = 0; k < VG; ++k) {
+      mean[k] = live ? a.mean[first * a.G + g[k]] : 0.0f;
+      rstd[k] = live ? a.rstd[first * a.G + g[k]] : 0.0f;
     }
-    auto hat = [&](int r, float* xh) {
+    // xhat and du; computed again for the result where there are several vectors to hold
+    auto both = [&](int r, float* xh, float* du) {
 #pragma unroll
       for (int k = 0; k < V; ++k) {
         float v = q[r].get(k);
         if constexpr (DROP) v = keep[r].kept(a.drop, k) ? v : 0.0f;
-        xh[k] = __builtin_fmaf(v, a.drop.scale, -mean[k]) * rstd[k];
+        xh[k] = __builtin_fmaf(v, a.drop.scale, -mean[MERGED ? 0 : k]) * rstd[MERGED ? 0 : k];
       }
+      grad_of<T, V>(a.act, w, b, e[r], xh, du);
     };
+    float xh[V], du[V];
 #pragma unroll
     for (int r = 0; r < R; ++r) {
       const int s = tm.row + r * a.step;
       if (live && s < a.S) {
         if constexpr (DROP) keep[r].draw(a.drop, (uint32_t)(i * a.S + s), tm.c);
-        float xh[V], du[V];
-        hat(r, xh);
-        grad_of<T, V>(a.act, w, b, e[r], xh, du);
+        both(r, xh, du);
 #pragma unroll
         for (int k = 0; k < V; ++k) {
           s1[k] += du[k];
@@ -269,15 +270,15 @@ __global__ __launch_bounds__(512) void k_norm_block_grad(NormArgs a) {
       s1[k] *= w[k];
       s2[k] *= w[k];
     }
-    column_sums<V>(a, tm, s1, merged, rows, parts, cols);
-    group_sums<V>(a, cols, merged, [&](int j, float s) { m1[j] = s * inv; });
-    column_sums<V>(a, tm, s2, merged, rows, parts, cols);
-    group_sums<V>(a, cols, merged, [&](int j, float s) { m2[j] = s * inv; });
+    column_sums<V>(a, tm, s1, MERGED, rows, parts, cols);
+    group_sums<V>(a, cols, MERGED, [&](int j, float s) { m1[j] = s * inv; });
+    column_sums<V>(a, tm, s2, MERGED, rows, parts, cols);
+    group_sums<V>(a, cols, MERGED, [&](int j, float s) { m2[j] = s * inv; });
     if (live) {
       T* dx = reinterpret_cast<T*>(a.dx) + i * a.dx_sn + tm.c;
-      float c1[V], c2[V];
+      float c1[VG], c2[VG];
 #pragma unroll
-      for (int k = 0; k < V; ++k) {
+      for (int k = 0; k < VG; ++k) {
         c1[k] = m1[g[k]];
         c2[k] = m2[g[k]];
       }
@@ -285,12 +286,11 @@ __global__ __launch_bounds__(512) void k_norm_block_grad(NormArgs a) {
       for (int r = 0; r < R; ++r) {
         const int s = tm.row + r * a.step;
         if (s < a.S) {
-          float xh[V], du[V];
-          hat(r, xh);
-          grad_of<T, V>(a.act, w, b, e[r], xh, du);
+          if constexpr (R > 1) both(r, xh, du);
 #pragma unroll
           for (int k = 0; k < V; ++k) {
-            du[k] = rstd[k] * a.drop.scale * (du[k] * w[k] - c1[k] - xh[k] * c2[k]);
+            const int kg = MERGED ? 0 : k;
+            du[k] = rstd[kg] * a.drop.scale * (du[k] * w[k] - c1[kg] - xh[k] * c2[kg]);
             if constexpr (DROP) du[k] = keep[r].kept(a.drop, k) ? du[k] : 0.0f;
           }
           store_own<T, V>(dx + s * a.dx_ss, du, tm.shift, false);
@@ -843,6 +843,8 @@ static NormArgs norm_args(const auv_norm* d, const NormPlan& p) {
   (bf16 ? (p.V == 8 ? (const void*)KERN<__bf16, 8, __VA_ARGS__> : (const void*)KERN<__bf16, 1, __VA_ARGS__>) \
         : (p.V == 4 ? (const void*)KERN<float, 4, __VA_ARGS__> : (const void*)KERN<float, 1, __VA_ARGS__>))
 #define AUV_CHUNK_KERNEL(KERN) (drop ? AUV_NORM_TYPES(KERN, true) : AUV_NORM_TYPES(KERN, false))
+#define AUV_BLOCK_GRAD(R, D) (merged ? AUV_NORM_TYPES(k_norm_block_grad, R, D, true) : AUV_NORM_TYPES(k_norm_block_grad, R, D, false))
+#define AUV_BLOCK_GRAD_DROP(R) (drop ? AUV_BLOCK_GRAD(R, true) : AUV_BLOCK_GRAD(R, false))
 #define AUV_BLOCK_DROP(KERN, R) (drop ? AUV_NORM_TYPES(KERN, R, true) : AUV_NORM_TYPES(KERN, R, false))
 #define AUV_BLOCK_KERNEL(KERN) \
   (p.R == 1 ? AUV_BLOCK_DROP(KERN, 1) : p.R == 2 ? AUV_BLOCK_DROP(KERN, 2) : AUV_BLOCK_DROP(KERN, 4))
@@ -930,8 +932,9 @@ int auv_norm_backward(const auv_norm* d, const auv_norm_grad* g, void* work, voi
     const size_t lds = d->groups <= teams && params ? (size_t)teams * 2 * p.m * sizeof(float) : 0;
     if (int rc = launch_norm_rows(fn, a, p, bf16, true, lds, s)) return rc;
   } else if (p.form == NORM_BLOCK) {
-    if (int rc = launch_kernel(fn, AUV_BLOCK_KERNEL(k_norm_block_grad), dim3(p.blocks), dim3(p.threads), args, block_lds(d, p), s))
-      return rc;
+    const bool merged = a.Cg % p.V == 0;
+    const void* k = p.R == 1 ? AUV_BLOCK_GRAD_DROP(1) : p.R == 2 ? AUV_BLOCK_GRAD_DROP(2) : AUV_BLOCK_GRAD_DROP(4);
+    if (int rc = launch_kernel(fn, k, dim3(p.blocks), dim3(p.threads), args, block_lds(d, p), s)) return rc;
   } else {
     const dim3 grid((unsigned)p.part_rows, p.tiles);
     const size_t lds = 2 * sizeof(float) * (256 / p.tile) * p.tile * p.V;
