@@ -380,32 +380,41 @@ __device__ __forceinline__ void join_lanes(float& n, float& m, float& M, int lan
   }
 }
 
-// U positions at a time: their loads are in flight together
-template <class T, int V, int U, class F>
+// U positions at a time: their loads are in flight together.  The second launch walks the chunk back (BACK): what the
+// first one read last is still in its XCD's L2, where the same workgroup of the same grid runs.
+template <class T, int V, int U, bool BACK, class F>
 __device__ __forceinline__ void walk(const Walker<T, V>& wk, const T* x, int64_t stride, F f) {
-  for (int s = wk.s0 + wk.row; s < wk.s1; s += U * wk.step) {
+  const int mine = wk.s1 - wk.s0 > wk.row ? (wk.s1 - wk.s0 - wk.row - 1) / wk.step + 1 : 0;   // positions of the thread
+  for (int n = 0; n < mine; n += U) {
     Vec<T, V> q[U];
+    int s[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      s[u] = wk.s0 + wk.row + (BACK ? mine - 1 - n - u : n + u) * wk.step;
+      if (n + u < mine) q[u].load(x + s[u] * stride);
+    }
 #pragma unroll
     for (int u = 0; u < U; ++u)
-      if (s + u * wk.step < wk.s1) q[u].load(x + (s + u * wk.step) * stride);
-#pragma unroll
-    for (int u = 0; u < U; ++u)
-      if (s + u * wk.step < wk.s1) f(s + u * wk.step, q[u]);
+      if (n + u < mine) f(s[u], q[u]);
   }
 }
-template <class T, int V, int U, class F>
+template <class T, int V, int U, bool BACK, class F>
 __device__ __forceinline__ void walk(const Walker<T, V>& wk, const T* x, int64_t stride, const T* dy, int64_t dstride, F f) {
-  for (int s = wk.s0 + wk.row; s < wk.s1; s += U * wk.step) {
+  const int mine = wk.s1 - wk.s0 > wk.row ? (wk.s1 - wk.s0 - wk.row - 1) / wk.step + 1 : 0;
+  for (int n = 0; n < mine; n += U) {
     Vec<T, V> q[U], e[U];
+    int s[U];
 #pragma unroll
-    for (int u = 0; u < U; ++u)
-      if (s + u * wk.step < wk.s1) {
-        q[u].load(x + (s + u * wk.step) * stride);
-        e[u].load(dy + (s + u * wk.step) * dstride);
+    for (int u = 0; u < U; ++u) {
+      s[u] = wk.s0 + wk.row + (BACK ? mine - 1 - n - u : n + u) * wk.step;
+      if (n + u < mine) {
+        q[u].load(x + s[u] * stride);
+        e[u].load(dy + s[u] * dstride);
       }
+    }
 #pragma unroll
     for (int u = 0; u < U; ++u)
-      if (s + u * wk.step < wk.s1) f(s + u * wk.step, q[u], e[u]);
+      if (n + u < mine) f(s[u], q[u], e[u]);
   }
 }
 
@@ -422,7 +431,7 @@ __global__ __launch_bounds__(256) void k_norm_stats(NormArgs a) {
 #pragma unroll
     for (int k = 0; k < V; ++k) first[k] = s1[k] = s2[k] = 0.0f;
     int count = 0;
-    walk<T, V, 4>(wk, wk.in(a.x, a.x_sn), a.x_ss, [&](int s, const Vec<T, V>& q) {
+    walk<T, V, 4, false>(wk, wk.in(a.x, a.x_sn), a.x_ss, [&](int s, const Vec<T, V>& q) {
       float v[V];
 #pragma unroll
       for (int k = 0; k < V; ++k) v[k] = q.get(k);
@@ -523,7 +532,7 @@ __global__ __launch_bounds__(256) void k_norm_apply(NormArgs a) {
     mean[k] = gm[max(ch.g[k], 0)];
     rstd[k] = gr[max(ch.g[k], 0)];
   }
-  walk<T, V, 4>(wk, wk.in(a.x, a.x_sn), a.x_ss, [&](int s, const Vec<T, V>& q) {
+  walk<T, V, 4, true>(wk, wk.in(a.x, a.x_sn), a.x_ss, [&](int s, const Vec<T, V>& q) {
     float v[V];
     Draws<V> keep;
     if constexpr (DROP) keep.draw(a.drop, (uint32_t)((int64_t)wk.i * a.S + s), wk.c);
@@ -553,7 +562,7 @@ __global__ __launch_bounds__(256) void k_norm_grad_sums(NormArgs a) {
       rstd[k] = a.rstd[(int64_t)wk.i * a.G + ch.g[k]];
       dw[k] = db[k] = 0.0f;
     }
-    walk<T, V, 2>(wk, wk.in(a.x, a.x_sn), a.x_ss, wk.in(a.dout, a.dout_sn), a.dout_ss, [&](int s, const Vec<T, V>& q, const Vec<T, V>& e) {
+    walk<T, V, 2, false>(wk, wk.in(a.x, a.x_sn), a.x_ss, wk.in(a.dout, a.dout_sn), a.dout_ss, [&](int s, const Vec<T, V>& q, const Vec<T, V>& e) {
       float xh[V], du[V];
       Draws<V> keep;
       if constexpr (DROP) keep.draw(a.drop, (uint32_t)((int64_t)wk.i * a.S + s), wk.c);
@@ -650,7 +659,7 @@ __global__ __launch_bounds__(256) void k_norm_grad_apply(NormArgs a) {
     m1[k] = g1[max(ch.g[k], 0)];
     m2[k] = g2[max(ch.g[k], 0)];
   }
-  walk<T, V, 2>(wk, wk.in(a.x, a.x_sn), a.x_ss, wk.in(a.dout, a.dout_sn), a.dout_ss, [&](int s, const Vec<T, V>& q, const Vec<T, V>& e) {
+  walk<T, V, 2, true>(wk, wk.in(a.x, a.x_sn), a.x_ss, wk.in(a.dout, a.dout_sn), a.dout_ss, [&](int s, const Vec<T, V>& q, const Vec<T, V>& e) {
     float xh[V], du[V];
     Draws<V> keep;
     if constexpr (DROP) keep.draw(a.drop, (uint32_t)((int64_t)wk.i * a.S + s), wk.c);

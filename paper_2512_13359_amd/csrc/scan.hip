@@ -305,9 +305,9 @@ static void scan_shape(const auv_scan* d, const auv_seq* const* seqs, int count,
   const int U = sh.V >= (grad ? 2 : 4) ? 4 : 8;   // scan_steps, scan_grad_steps
   // Waves per workgroup until there are eight per CU (4095 x 23 fp32 columns x 500 steps, 736 tiles, forward and backward: one wave
   // 160 and 355 us, two 145 and 260, four 142 and 243; where there are eight anyway one wave is best, 16384 x 64 columns x 64 steps: 81, two
-  // waves 88).
+  // waves 88); four per CU do for accesses of 16 bytes (4096 x 64 fp32 columns x 128: one wave 73 and 149, two 79 and 157).
   sh.W = 1;
-  while (sh.W < SCAN_WAVES && (int64_t)a.tiles * sh.W < 8 * cus && sh.W * U < d->T) sh.W *= 2;
+  while (sh.W < SCAN_WAVES && (int64_t)a.tiles * sh.W < (sh.V == 4 && d->type == AUV_FP32 ? 4 : 8) * cus && sh.W * U < d->T) sh.W *= 2;
   const int span = sh.W * U, rounds = (d->T - 1) / span + 1;
   // Steps split over workgroups where there is less than one per CU, up to two per CU: reads gate and input (or dout) twice.
   // 2048 columns x 4096 steps: whole 201 and 398 us, split in 16 30 and 43, in 32 25 and 33; 16384 columns x 1024 steps: whole 54 and

@@ -231,24 +231,29 @@ def test_scan_broadcast_inputs_and_absent_gradients():
     assert torch.equal(one, scan_forward(x[:1].expand(T, n, c).contiguous(), x, kind="decay")[0])
 
 
-def test_scan_steps_equal_one_run():
-    """T calls of one step, the state updated in place, give the run of T steps."""
+def test_scan_steps_in_place():
+    """A controller's single steps: the state updated in place by every call, one captured step replayed."""
     require_gpu()
     from paper_2512_13359_amd import _abi as A
-    from paper_2512_13359_amd import scan_forward
     T, n, c = 12, 256, 64
     gate, x, done, _, h0, _, _ = scan_inputs(T, n, c, "bf16", "sigmoid", "tnc", "d", 4)
-    h, last = scan_forward(gate, x, done=done, h0=h0)
-    s = h0.clone()
-    out = torch.empty(1, n, c, dtype=x.dtype, device="cuda")
+    delta = (np.abs(f64(gate)) + 24) * U
+    wh, wl, bh, bl = L.scan(f64(gate), f64(x), done=host(done), h0=f64(h0), delta=delta)
+    z, v, d, out, s = gate[0].clone(), x[0].clone(), done[0].clone(), torch.empty_like(x[0]), h0.clone()
+    step = A.AuvScan(1, n, c, A.AUV_BF16, A.AUV_SCAN_SIGMOID, z.data_ptr(), n * c, c, 1, v.data_ptr(), n * c, c, 1,
+                     out.data_ptr(), n * c, c, 1, d.data_ptr(), None, s.data_ptr(), c, 1, s.data_ptr(), c, 1)
+    assert A.auv_scan_work_bytes(step) == 0
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        A.auv_scan_forward(step, None)
+    hs = []
     for t in range(T):
-        d = A.AuvScan(1, n, c, A.AUV_BF16, 0, gate[t].data_ptr(), n * c, c, 1, x[t].data_ptr(), n * c, c, 1, out.data_ptr(),
-                      n * c, c, 1, done[t].data_ptr(), None, s.data_ptr(), c, 1, s.data_ptr(), c, 1)
-        A.auv_scan_forward(d, None)
-        one, s2 = scan_forward(gate[t:t + 1], x[t:t + 1], done=done[t:t + 1], h0=s if t == 0 else prev)
-        prev = s2 if t else scan_forward(gate[:1], x[:1], done=done[:1], h0=h0)[1]
-        assert np.abs(f64(out[0]) - f64(h[t])).max() <= 2 ** -7 * max(1.0, np.abs(f64(h[t])).max())
-    assert np.abs(f64(s) - f64(last)).max() <= 64 * U * max(1.0, np.abs(f64(last)).max())
+        z.copy_(gate[t]), v.copy_(x[t]), d.copy_(done[t])
+        graph.replay()
+        hs.append(out.clone())
+    within(torch.stack(hs), wh, bh + HALF["bf16"] * (np.abs(wh) + bh), "h")
+    within(s, wl, bl + U * np.abs(wl), "state")
 
 
 # ---------------------------------------------------------------------------- norm --
@@ -397,7 +402,6 @@ def test_dropout(n, s, c, pitch, typ):
     shape = (n, s, c) if s > 1 else (n, c)
     x = torch.randn((*shape[:-1], c + pitch), generator=g, device="cuda").to(TYPES[typ])[..., :c]
     add = torch.randn(shape, generator=g, device="cuda").to(TYPES[typ])
-    x.view(-1)[0] if x.is_contiguous() else None
     for p in (0.0, 0.1, 0.5, 0.9):
         d = make_drop(p, 0x1122334455667788, 3, 9, 50)
         factor = L.drop_factor(n * s, c, d.drop, 0x1122334455667788, 3, 9, 50).reshape(shape)
@@ -532,3 +536,44 @@ def test_stream_argument_and_two_streams_at_once():
     torch.cuda.synchronize()
     for a, b in outs:
         assert all(torch.equal(p, q) for p, q in zip(a, want)) and all(torch.equal(p, q) for p, q in zip(b, wn))
+
+
+def test_offsets_beyond_32_bits():
+    """Tensors of more than 2^31 elements: their ends equal the same calls on the ends alone."""
+    require_gpu()
+    from paper_2512_13359_amd import dropout, make_drop, norm_backward, norm_forward, scan_backward, scan_forward
+    g = torch.Generator(device="cuda")
+    g.manual_seed(0)
+    rand = lambda *s: torch.empty(s, dtype=torch.bfloat16, device="cuda").normal_(generator=g)  # noqa: E731
+    T, n, c, tail = 33000, 1024, 64, 10
+    announce("scan of 2.2e9 elements")
+    gate, x = rand(T, n, c), rand(T, n, c)
+    done = torch.zeros(T, n, device="cuda")
+    done[T - tail - 1] = 1.0                    # the last steps are an episode of their own
+    assert gate.numel() > 2 ** 31
+    h, last = scan_forward(gate, x, done=done)
+    zt, xt = gate[-tail:], x[-tail:]
+    delta = (np.abs(f64(zt)) + 24) * U
+    wh, wl, bh, bl = L.scan(f64(zt), f64(xt), delta=delta)
+    within(h[-tail:], wh, bh + HALF["bf16"] * (np.abs(wh) + bh), "h")
+    within(last, wl, bl + U * np.abs(wl), "last")
+    dgate, dx, _ = scan_backward(gate, x, h, dout=x, done=done)
+    wg, wx, _, bg, bx, _ = L.scan_grad(f64(zt), f64(xt), f64(h[-tail:]), f64(xt), None, delta=delta)
+    within(dgate[-tail:], wg, bg + HALF["bf16"] * (np.abs(wg) + bg), "dgate")
+    within(dx[-tail:], wx, bx + HALF["bf16"] * (np.abs(wx) + bx), "dx")
+    del h, dgate, dx, gate
+    announce("norm and dropout of 2.2e9 elements")
+    for shape in ((T * 128, 512), (2, T * 32, 1024)):       # the rows form, the chunk form (two samples)
+        v = x.view(shape)
+        y, mean, rstd = norm_forward(v, 1, act="silu")
+        d, _, _ = norm_backward(v, 1, mean, rstd, v, act="silu")
+        end = v[-50:] if len(shape) == 2 else v[1:]
+        y2, mean2, rstd2 = norm_forward(end, 1, act="silu")
+        d2, _, _ = norm_backward(end, 1, mean2, rstd2, end, act="silu")
+        # another number of chunks joins the statistics in another order: a few ulps, then one step of bf16
+        near = lambda a, b: float((a.float() - b.float()).abs().max()) <= 2.0 ** -7 * float(b.float().abs().max())  # noqa: E731
+        assert near(y[-len(end):][..., -40:, :], y2[..., -40:, :]) and near(d[-len(end):][..., -40:, :], d2[..., -40:, :])
+        del y, d, y2, d2
+    v = x.view(T * 256, 256)
+    y = dropout(v, make_drop(0.5, 9))
+    assert torch.equal(y[-1000:], dropout(v[-1000:], make_drop(0.5, 9, row0=T * 256 - 1000)))
