@@ -474,7 +474,7 @@ __device__ __forceinline__ void report_status(uint32_t* status, uint32_t nonfini
 // DPP lane moves for reductions (GCN row = 16 lanes): rotate right within each row, and
 // broadcast lane 15 / 31 into the following row(s) (rows outside row_mask read zero).
 constexpr int DPP_ROW_ROR4 = 0x124, DPP_ROW_ROR8 = 0x128, DPP_ROW_ROR12 = 0x12C, DPP_ROW_BCAST15 = 0x142,
-              DPP_ROW_BCAST31 = 0x143, DPP_ROW_MIRROR = 0x140, DPP_ROW_HALF_MIRROR = 0x141;
+              DPP_ROW_BCAST31 = 0x143;
 constexpr int DPP_QUAD_SWAP1 = 0xB1, DPP_QUAD_SWAP2 = 0x4E;   // quad_perm [1,0,3,2], [2,3,0,1]
 
 template <int CTRL, int ROW_MASK = 0xF>

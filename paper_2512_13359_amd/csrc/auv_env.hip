@@ -32,15 +32,6 @@ int check_launch(const char* what) {
   return AUV_OK;
 }
 
-int launch_kernel(const char* fn, const void* kernel, dim3 grid, dim3 block, void** args, size_t lds, hipStream_t s) {
-  const hipError_t e = hipLaunchKernel(kernel, grid, block, args, lds, s);
-  if (e != hipSuccess) {
-    (void)hipGetLastError();
-    return set_error(AUV_ELAUNCH, "%s: launch failed: %s", fn, hipGetErrorString(e));
-  }
-  return AUV_OK;
-}
-
 // ------------------------------------------------------------------------ kernels --
 
 __global__ __launch_bounds__(256) void k_reset(VehArgs V, EnvArgs E) {

@@ -25,8 +25,6 @@ namespace auv {
 int set_error(int code, const char* fmt, ...);
 bool aligned16(const void* p);
 int check_launch(const char* what);
-// a kernel by its address; `fn` is the entry point named in the error
-int launch_kernel(const char* fn, const void* kernel, dim3 grid, dim3 block, void** args, size_t lds, hipStream_t s);
 
 inline int groups_of(int n) { return (n + 63) / 64; }
 

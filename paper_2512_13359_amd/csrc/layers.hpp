@@ -5,7 +5,19 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include "auv_internal.hpp"
+
 namespace auv {
+
+// A kernel by its address; `fn` is the entry point named in the error.
+inline int launch_kernel(const char* fn, const void* kernel, dim3 grid, dim3 block, void** args, size_t lds, hipStream_t s) {
+  const hipError_t e = hipLaunchKernel(kernel, grid, block, args, lds, s);
+  if (e != hipSuccess) {
+    (void)hipGetLastError();
+    return set_error(AUV_ELAUNCH, "%s: launch failed: %s", fn, hipGetErrorString(e));
+  }
+  return AUV_OK;
+}
 
 // ------------------------------------------------------------------ vector accesses --
 // V elements of a row as one access of up to 16 bytes.  Rows start at any multiple of the

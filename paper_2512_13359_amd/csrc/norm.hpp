@@ -37,6 +37,8 @@ struct NormPlan {
   int64_t part_rows;           // backward: partial rows of [2][C] floats
 };
 
+constexpr int DPP_ROW_MIRROR = 0x140, DPP_ROW_HALF_MIRROR = 0x141;   // lane i of 16 from 15 - i, of 8 from 7 - i
+
 // Sum over a team of LANES lanes (a power of two), every lane gets it: moves within rows of 16 lanes, then lane swaps.
 template <int LANES> __device__ __forceinline__ float lanes_sum(float v) {
   if constexpr (LANES > 1) v += dpp_move<DPP_QUAD_SWAP1>(v);
