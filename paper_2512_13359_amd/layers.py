@@ -142,8 +142,11 @@ def scan_backward(gate, x, h, *, dout=None, dh_last=None, kind="sigmoid", done=N
         _like(fn, "dout", dout, x.shape, x.dtype, x.device)
     if dh_last is not None:
         _like(fn, "dh_last", dh_last, x.shape[1:], torch.float32, x.device)
-    for o in out or ():
-        _like(fn, "out", o, x.shape, x.dtype, x.device)
+    if out is not None:
+        if len(out) != 2:
+            _refuse(fn, "out must be the pair (dgate, dx)")
+        for o in out:
+            _like(fn, "out", o, x.shape, x.dtype, x.device)
     if not _here(fn, x, stream):
         with _Moved(x, stream):
             return scan_backward(gate, x, h, dout=dout, dh_last=dh_last, kind=kind, done=done, lens=lens, h0=h0, out=out)
