@@ -727,10 +727,8 @@ static bool plan_rows(const auv_norm* d, bool dense, bool backward, NormPlan& p)
   return true;
 }
 
-// Up to four vectors per thread of at most 512; several samples per workgroup where one leaves threads idle.  Workgroups per CU,
-// each for many samples, keep weights and sums: 262144 x 8 x 3 bf16 in 3 groups, forward 6 per CU 44 us, 4 60, 16 47;
-// backward 4 per CU 67, 6 52, and 30000 x 8 x 32 in 8 groups 44 and 49.
-static bool plan_block(const auv_norm* d, bool backward, NormPlan& p) {
+// Up to four vectors per thread of at most 256, or 512; several samples per workgroup where one leaves threads idle.
+static bool plan_block(const auv_norm* d, NormPlan& p) {
   const int full = d->type == AUV_BF16 ? 8 : 4;
   p.form = NORM_BLOCK;
   p.V = d->c >= full ? full : 1;
@@ -738,22 +736,55 @@ static bool plan_block(const auv_norm* d, bool backward, NormPlan& p) {
   if (vecs > 512 || all > 4 * 512) return false;
   p.tile = (int)vecs;
   p.tiles = 1;
-  p.threads = all <= 4 * 256 && vecs <= 256 ? 256 : 512;
-  if (all <= p.threads) {
-    p.step = d->s;
-    p.pack = (int)std::min<int64_t>(d->n, p.threads / all);
-    p.R = 1;
-  } else {
-    p.step = p.threads / p.tile;
-    p.pack = 1;
-    const int need = (d->s - 1) / p.step + 1;
-    if (need > 4) return false;
-    p.R = need > 2 ? 4 : need;
-  }
-  const int64_t want = (d->n - 1) / p.pack + 1;
-  p.blocks = (int)std::min<int64_t>(want, (int64_t)compute_units() * (backward ? 4 : 6));
+  p.pack = (int)std::min<int64_t>(d->n, std::max<int64_t>(1, 256 / all));
+  bool fits = false;
+  for (int most = 256; most <= 512 && !fits; most *= 2)
+    for (p.R = 1; p.R <= 4; p.R *= 2)
+      if ((fits = p.tile * ((d->s - 1) / p.R + 1) <= most)) break;
+  if (!fits) return false;
+  p.step = (d->s - 1) / p.R + 1;
+  p.threads = (p.pack * p.step * p.tile + 63) / 64 * 64;
+  // 24 waves per CU at most (262144 x 8 x 3 bf16 in 3 groups, forward: 43 us, 32 waves 55, 16 58); launch_block takes as many
+  // of them as are resident
+  p.blocks = (int)std::min<int64_t>((d->n - 1) / p.pack + 1, (int64_t)compute_units() * (1536 / p.threads));
   p.part_rows = p.blocks;
   return true;
+}
+
+#define AUV_NORM_TYPES(KERN, ...)                                                                               \
+  (bf16 ? (p.V == 8 ? (const void*)KERN<__bf16, 8, __VA_ARGS__> : (const void*)KERN<__bf16, 1, __VA_ARGS__>) \
+        : (p.V == 4 ? (const void*)KERN<float, 4, __VA_ARGS__> : (const void*)KERN<float, 1, __VA_ARGS__>))
+#define AUV_CHUNK_KERNEL(KERN) (drop ? AUV_NORM_TYPES(KERN, true) : AUV_NORM_TYPES(KERN, false))
+#define AUV_BLOCK_GRAD(R, D) (merged ? AUV_NORM_TYPES(k_norm_block_grad, R, D, true) : AUV_NORM_TYPES(k_norm_block_grad, R, D, false))
+#define AUV_BLOCK_GRAD_DROP(R) (drop ? AUV_BLOCK_GRAD(R, true) : AUV_BLOCK_GRAD(R, false))
+#define AUV_BLOCK_DROP(KERN, R) (drop ? AUV_NORM_TYPES(KERN, R, true) : AUV_NORM_TYPES(KERN, R, false))
+#define AUV_BLOCK_KERNEL(KERN) \
+  (p.R == 1 ? AUV_BLOCK_DROP(KERN, 1) : p.R == 2 ? AUV_BLOCK_DROP(KERN, 2) : AUV_BLOCK_DROP(KERN, 4))
+
+static size_t block_lds(const auv_norm* d, const NormPlan& p) {   // see the kernels: groups, columns, parts, rows
+  const size_t cols = (size_t)p.pack * d->c;
+  return sizeof(float) * (2 * (size_t)p.pack * d->groups + cols + p.threads + (p.step > 1 ? cols * p.step : 0));
+}
+
+// The block form's launch, by workgroups that are all resident: each keeps weights and sums over its samples, and one more
+// round of a few would last as long as all others (11803 x 8 x 160 fp32 in 32 groups, backward: 12 waves per CU, which the
+// registers hold, 78 us, 16 107).
+static int launch_block(const char* fn, const auv_norm* d, NormPlan& p, NormArgs& a, bool grad, hipStream_t s) {
+  const bool bf16 = d->type == AUV_BF16, drop = d->drop && d->drop->drop, merged = a.Cg % p.V == 0;
+  const void* k = !grad ? AUV_BLOCK_KERNEL(k_norm_block)
+                  : p.R == 1 ? AUV_BLOCK_GRAD_DROP(1) : p.R == 2 ? AUV_BLOCK_GRAD_DROP(2) : AUV_BLOCK_GRAD_DROP(4);
+  const size_t lds = block_lds(d, p);
+  if (p.blocks > compute_units()) {
+    int resident = 0;
+    if (hipOccupancyMaxActiveBlocksPerMultiprocessor(&resident, k, p.threads, lds) != hipSuccess || resident < 1) {
+      (void)hipGetLastError();
+      resident = 1;
+    }
+    p.blocks = std::min(p.blocks, compute_units() * resident);
+    p.part_rows = a.part_rows = p.blocks;
+  }
+  void* args[1] = {&a};
+  return launch_kernel(fn, k, dim3(p.blocks), dim3(p.threads), args, lds, s);
 }
 
 // Chunks of at least four passes of a workgroup, two workgroups per CU where the positions allow (4 x 8192 x 512 bf16 in 32
@@ -778,7 +809,7 @@ static int plan_chunks(const char* fn, const auv_norm* d, NormPlan& p) {
 
 static int plan(const char* fn, const auv_norm* d, bool dense, bool backward, NormPlan& p) {
   p = NormPlan{};
-  if (plan_rows(d, dense, backward, p) || plan_block(d, backward, p)) return AUV_OK;
+  if (plan_rows(d, dense, backward, p) || plan_block(d, p)) return AUV_OK;
   return plan_chunks(fn, d, p);
 }
 
@@ -848,21 +879,6 @@ static NormArgs norm_args(const auv_norm* d, const NormPlan& p) {
   return a;
 }
 
-#define AUV_NORM_TYPES(KERN, ...)                                                                               \
-  (bf16 ? (p.V == 8 ? (const void*)KERN<__bf16, 8, __VA_ARGS__> : (const void*)KERN<__bf16, 1, __VA_ARGS__>) \
-        : (p.V == 4 ? (const void*)KERN<float, 4, __VA_ARGS__> : (const void*)KERN<float, 1, __VA_ARGS__>))
-#define AUV_CHUNK_KERNEL(KERN) (drop ? AUV_NORM_TYPES(KERN, true) : AUV_NORM_TYPES(KERN, false))
-#define AUV_BLOCK_GRAD(R, D) (merged ? AUV_NORM_TYPES(k_norm_block_grad, R, D, true) : AUV_NORM_TYPES(k_norm_block_grad, R, D, false))
-#define AUV_BLOCK_GRAD_DROP(R) (drop ? AUV_BLOCK_GRAD(R, true) : AUV_BLOCK_GRAD(R, false))
-#define AUV_BLOCK_DROP(KERN, R) (drop ? AUV_NORM_TYPES(KERN, R, true) : AUV_NORM_TYPES(KERN, R, false))
-#define AUV_BLOCK_KERNEL(KERN) \
-  (p.R == 1 ? AUV_BLOCK_DROP(KERN, 1) : p.R == 2 ? AUV_BLOCK_DROP(KERN, 2) : AUV_BLOCK_DROP(KERN, 4))
-
-static size_t block_lds(const auv_norm* d, const NormPlan& p) {   // see the kernels: groups, columns, parts, rows
-  const size_t cols = (size_t)p.pack * d->c;
-  return sizeof(float) * (2 * (size_t)p.pack * d->groups + cols + p.threads + (p.step > 1 ? cols * p.step : 0));
-}
-
 // groups that a tile of channels can hold a part of
 static size_t tile_groups(const auv_norm* d, const NormPlan& p) {
   const int wide = std::min(p.tile * p.V, d->c), cg = d->c / d->groups;
@@ -901,8 +917,7 @@ int auv_norm_forward(const auv_norm* d, const auv_rows* y, void* work, void* str
   void* args[1] = {&a};
   hipStream_t s = (hipStream_t)stream;
   if (p.form == NORM_ROWS) return launch_norm_rows(fn, a, p, bf16, false, 0, s);
-  if (p.form == NORM_BLOCK)
-    return launch_kernel(fn, AUV_BLOCK_KERNEL(k_norm_block), dim3(p.blocks), dim3(p.threads), args, block_lds(d, p), s);
+  if (p.form == NORM_BLOCK) return launch_block(fn, d, p, a, false, s);
   const dim3 grid((unsigned)p.part_rows, p.tiles);
   const size_t lds = 2 * sizeof(float) * (256 / p.tile) * p.tile * p.V;
   if (int rc = launch_kernel(fn, AUV_CHUNK_KERNEL(k_norm_stats), grid, dim3(256), args, lds, s)) return rc;
@@ -941,9 +956,7 @@ int auv_norm_backward(const auv_norm* d, const auv_norm_grad* g, void* work, voi
     const size_t lds = d->groups <= teams && params ? (size_t)teams * 2 * p.m * sizeof(float) : 0;
     if (int rc = launch_norm_rows(fn, a, p, bf16, true, lds, s)) return rc;
   } else if (p.form == NORM_BLOCK) {
-    const bool merged = a.Cg % p.V == 0;
-    const void* k = p.R == 1 ? AUV_BLOCK_GRAD_DROP(1) : p.R == 2 ? AUV_BLOCK_GRAD_DROP(2) : AUV_BLOCK_GRAD_DROP(4);
-    if (int rc = launch_kernel(fn, k, dim3(p.blocks), dim3(p.threads), args, block_lds(d, p), s)) return rc;
+    if (int rc = launch_block(fn, d, p, a, true, s)) return rc;
   } else {
     const dim3 grid((unsigned)p.part_rows, p.tiles);
     const size_t lds = 2 * sizeof(float) * (256 / p.tile) * p.tile * p.V;

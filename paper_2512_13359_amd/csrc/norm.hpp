@@ -1,6 +1,6 @@
 // Group norm: what its three forms share.
-//   rows    a group is up to 1024 contiguous numbers (one position, or one group over dense positions): in the registers
-//           of 1 to 64 lanes (norm_rows.hip)
+//   rows    a group is up to 1024 contiguous numbers (one position, or one group over dense positions): in
+//           the registers of 1 to 64 lanes (norm_rows.hip)
 //   block   a sample is up to a few thousand vectors: in the registers of a workgroup (norm.hip)
 //   chunks  larger samples: statistics by one launch, applied by the next, which reads the sample again (norm.hip)
 #pragma once

@@ -28,8 +28,12 @@ template <class T, int V, int NV> struct RowTeam {
       keep.draw(a.drop, (uint32_t)sample, g * a.m + at[j]);
       return;
     }
-    uint32_t bits = 0;   // the vector may go over several positions
     int pos = at[j] / a.C, c = at[j] % a.C;
+    if (a.C % V == 0) {
+      keep.draw(a.drop, (uint32_t)(sample * a.S + pos), c);
+      return;
+    }
+    uint32_t bits = 0;   // the vector may go over several positions
     for (int k = 0; k < V;) {
       const int run = min(V - k, min(a.C - c, 8 - (c & 7)));
       bits |= (drop_bits(a.drop, (uint32_t)(sample * a.S + pos), c >> 3) >> (c & 7) & ((1u << run) - 1u)) << k;
