@@ -28,6 +28,8 @@ __device__ __forceinline__ void grad_of(int act, const float* w, const float* b,
 // ------------------------------------------------------------------- block form -------
 // A workgroup holds `pack` samples at a time in registers, R vectors per thread: a thread keeps V channels and takes
 // every step-th position of its sample.  Sums go from threads to columns (channels of a sample) to groups through LDS.
+// Read and written once; bound by the chain of a pass (load, two sums of three barriers each, store) where samples are small:
+// 30000 x 8 x 32 bf16 in 8 groups, forward 18 us (1.7 TB/s) and backward 32; 20000 x 2000 fp32 79 (4.1) and 118 (4.1).
 template <class T, int V, int R> struct BlockTeam {
   bool on;
   int c, shift, p, row, q;   // channel, sample of the pass, first position, row of LDS
@@ -314,7 +316,8 @@ __global__ __launch_bounds__(512) void k_norm_block_grad(NormArgs a) {
 // ------------------------------------------------------------------ chunk form -------
 // A workgroup walks over a chunk of a sample's positions and a tile of its channels, a thread keeping V channels.  The
 // first launch leaves every chunk's and tile's share of each group's statistics, [n][chunk][tile][G]; the second joins a
-// group's shares in its first instructions.
+// group's shares in its first instructions.  Bound by HBM and the second read: 32 x 4096 x 256 bf16 in 32 groups with SiLU, 13 us for the
+// statistics (5.2 TB/s) and 26 for the rest (5.2); backward 68.
 template <class T, int V> struct Walker {
   bool on;
   int i, chunk, c, shift, row, step, s0, s1;   // sample, chunk, channel, positions [s0, s1) from s0 + row on by `step`
