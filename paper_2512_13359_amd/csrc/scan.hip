@@ -227,6 +227,13 @@ int launch_scan_forward(const ScanArgs& a, const ScanShape& sh, bool bf16, bool 
 
 // ----------------------------------------------------------------------- shapes -------
 
+// Whether the strides are none below zero and no axis spans 2^44 elements or more.
+static bool spans(const int64_t* stride, const int64_t* size, int n) {
+  for (int k = 0; k < n; ++k)
+    if (stride[k] < 0 || (size[k] > 1 && stride[k] > ((int64_t)1 << 44) / (size[k] - 1))) return false;
+  return true;
+}
+
 // Whether no two elements of an output share memory: each axis steps over all of the ones inside it.
 static bool disjoint(const int64_t* stride, const int64_t* size, int n) {
   int order[3] = {0, 1, 2};
@@ -245,8 +252,7 @@ static int check_state(const char* fn, const char* name, const auv_seq_state& s,
   if (!s.p) return AUV_OK;
   if (reinterpret_cast<uintptr_t>(s.p) & 3u) return set_error(AUV_EINVAL, "%s: '%s' is not 4-byte aligned", fn, name);
   const int64_t st[2] = {s.sn, s.sc}, size[2] = {d->n, d->c};
-  for (int k = 0; k < 2; ++k)
-    if (st[k] < 0 || st[k] > ((int64_t)1 << 40)) return set_error(AUV_EINVAL, "%s: '%s' has a stride outside [0, 2^40]", fn, name);
+  if (!spans(st, size, 2)) return set_error(AUV_EINVAL, "%s: '%s' has a negative stride or spans 2^44 elements or more", fn, name);
   if (output && !disjoint(st, size, 2)) return set_error(AUV_EINVAL, "%s: elements of '%s' share memory", fn, name);
   return AUV_OK;
 }
@@ -256,9 +262,7 @@ static int check_seq(const char* fn, const char* name, const auv_seq& s, const a
   if (reinterpret_cast<uintptr_t>(s.p) & (d->type == AUV_BF16 ? 1u : 3u))
     return set_error(AUV_EINVAL, "%s: '%s' is not aligned to its elements", fn, name);
   const int64_t st[3] = {s.st, s.sn, s.sc}, size[3] = {d->T, d->n, d->c};
-  for (int k = 0; k < 3; ++k)
-    if (st[k] < 0 || (size[k] - 1) * (st[k] >> 20) > ((int64_t)1 << 24))
-      return set_error(AUV_EINVAL, "%s: '%s' has a negative stride or spans 2^44 elements or more", fn, name);
+  if (!spans(st, size, 3)) return set_error(AUV_EINVAL, "%s: '%s' has a negative stride or spans 2^44 elements or more", fn, name);
   if (output && !disjoint(st, size, 3)) return set_error(AUV_EINVAL, "%s: elements of '%s' share memory", fn, name);
   return AUV_OK;
 }

@@ -372,6 +372,26 @@ def test_norm_far_from_zero(s, c, groups):
     check_norm(5, s, c, groups, "fp32", "none", shift=1500.0, seed=8)
 
 
+@pytest.mark.parametrize("n, s, c, groups", [(40, 1, 32, 1), (3, 5, 24, 3), (2, 3000, 16, 2)])
+def test_norm_weight_or_bias_alone(n, s, c, groups):
+    """A parameter that is not given stands for 1 or 0 and has no gradient; the other's is the same."""
+    require_gpu()
+    from paper_2512_13359_amd import norm_backward, norm_forward
+    g = torch.Generator(device="cuda")
+    g.manual_seed(1)
+    x, dy = (torch.randn(n, s, c, generator=g, device="cuda") for _ in range(2))
+    p, one, zero = torch.randn(c, generator=g, device="cuda"), torch.ones(c, device="cuda"), torch.zeros(c, device="cuda")
+    for alone, both in ((dict(weight=p), dict(weight=p, bias=zero)), (dict(bias=p), dict(weight=one, bias=p)), ({}, dict(weight=one, bias=zero))):
+        y, mean, rstd = norm_forward(x, groups, act="silu", **alone)
+        y2, _, _ = norm_forward(x, groups, act="silu", **both)
+        assert torch.equal(y, y2)
+        a = norm_backward(x, groups, mean, rstd, dy, act="silu", **alone)
+        b = norm_backward(x, groups, mean, rstd, dy, act="silu", **both)
+        assert torch.equal(a[0], b[0])
+        for k, name in ((1, "weight"), (2, "bias")):
+            assert torch.equal(a[k], b[k]) if name in alone else a[k] is None
+
+
 def test_norm_statistics_of_constant_and_empty_groups():
     """A group of one value has variance zero, and so has one whose every element is dropped."""
     require_gpu()

@@ -25,7 +25,7 @@ def _grad(A, **kw):
     (dict(T=0), "T"), (dict(n=-1), "T"), (dict(c=0), "T"), (dict(n=1 << 20, c=1 << 20), "2^30"), (dict(type=2), "type"),
     (dict(kind=7), "kind"), (dict(gate=None), "gate"), (dict(x=None), "x"), (dict(h=None), "h"), (dict(x=P + 2), "aligned"),
     (dict(h_st=8), "share"), (dict(h_sc=0), "share"), (dict(h=P), "input"), (dict(x_st=-1), "negative"),
-    (dict(x_st=1 << 50), "2^44"), (dict(h0=P + 1), "h0"), (dict(last=P, last_sn=0, last_sc=1), "last"),
+    (dict(x_st=1 << 50), "2^44"), (dict(h0=P, h0_sn=1 << 44), "2^44"), (dict(last=P, last_sn=-8, last_sc=1), "negative"), (dict(h0=P + 1), "h0"), (dict(last=P, last_sn=0, last_sc=1), "last"),
     (dict(done=P + 3), "done"), (dict(h0=P, h0_sn=8, h0_sc=1, last=P, last_sn=1, last_sc=3), "last")])
 def test_scan_forward_refuses(change, word):
     from paper_2512_13359_amd import _abi as A
