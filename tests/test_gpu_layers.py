@@ -231,6 +231,29 @@ def test_scan_broadcast_inputs_and_absent_gradients():
     assert torch.equal(one, scan_forward(x[:1].expand(T, n, c).contiguous(), x, kind="decay")[0])
 
 
+def test_scan_rows_far_apart():
+    """Sequences further apart than 32 bits of bytes, next to ones that are not."""
+    require_gpu()
+    from paper_2512_13359_amd import scan_backward, scan_forward
+    T, n, c, far = 40, 3, 24, 1_200_000_000
+    g = torch.Generator(device="cuda")
+    g.manual_seed(2)
+    gate, x, dout = (torch.randn(T, n, c, generator=g, device="cuda").bfloat16() for _ in range(3))
+    room = torch.empty(n * far, dtype=torch.bfloat16, device="cuda")
+    wide = room.as_strided((T, n, c), (c, far, 1))
+    wide.copy_(x)
+    h, last = scan_forward(gate, x)
+    dgate, dx, dh0 = scan_backward(gate, x, h, dout=dout)
+    a = scan_forward(gate, wide, out=torch.empty_like(h))
+    b = scan_backward(gate, wide, h, dout=dout, out=(torch.empty_like(dgate), torch.empty_like(dx)))
+    within(a[0], f64(h), 2.0 ** -7 * np.abs(f64(h)), "h")      # one step of bf16 where the launch's shape adds in another order
+    within(a[1], f64(last), 2.0 ** -16 * (1 + np.abs(f64(last))), "last")
+    for p, q, what in zip(b, (dgate, dx, dh0), ("dgate", "dx", "dh0")):
+        within(p, f64(q), 2.0 ** -7 * np.abs(f64(q)) + 2.0 ** -16, what)
+    out = room.as_strided((T, n, c), (c, far, 1), 7 * c * T)   # and an output there
+    assert torch.equal(scan_forward(gate, wide, out=out)[0], a[0])
+
+
 def test_scan_steps_in_place():
     """A controller's single steps: the state updated in place by every call, one captured step replayed."""
     require_gpu()
