@@ -523,8 +523,9 @@ typedef struct {
 } auv_scan_grad;
 
 /* Bytes of device workspace of auv_scan_forward (g NULL) or auv_scan_backward on these tensors:
- * 0 unless the columns are too few for the chip and the steps many (work may then be NULL); -1 on
- * bad arguments. */
+ * 0 unless the columns are too few for the chip and the steps AUV_SCAN_SPLIT_STEPS at least (work may
+ * then be NULL); -1 on bad arguments. */
+#define AUV_SCAN_SPLIT_STEPS 128
 int64_t auv_scan_work_bytes(const auv_scan* s, const auv_scan_grad* g);
 int auv_scan_forward(const auv_scan* s, void* work, void* stream);
 int auv_scan_backward(const auv_scan* s, const auv_scan_grad* g, void* work, void* stream);

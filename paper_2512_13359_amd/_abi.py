@@ -25,6 +25,7 @@ AUV_CONV_UNIFORM, AUV_CONV_UNIFORM_OPEN0, AUV_CONV_AFFINE, AUV_CONV_BF16 = 0, 1,
 AUV_PROBE_EXP, AUV_PROBE_RCP, AUV_PROBE_FMA, AUV_PROBE_MFMA_BF16 = 0, 1, 2, 3
 AUV_FP32, AUV_BF16 = 0, 1
 AUV_SCAN_SIGMOID, AUV_SCAN_DECAY = 0, 1
+AUV_SCAN_SPLIT_STEPS = 128
 AUV_ACTIVATION_NONE, AUV_ACTIVATION_RELU, AUV_ACTIVATION_SILU, AUV_ACTIVATION_TANH = 0, 1, 2, 3
 OBS_DIM, ACT_DIM, STATE_DIM, PARAM_DIM, HIDDEN, ENVS_PER_GROUP = 23, 8, 13, 24, 256, 64
 

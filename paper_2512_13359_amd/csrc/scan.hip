@@ -322,7 +322,8 @@ static void scan_shape(const auv_scan* d, const auv_seq* const* seqs, int count,
   // 105, in four 39 and 54, in eight 46 and 59; 32768 columns (256 tiles): whole 57 and 115, in two 64 and 107.
   sh.K = 1;
   const bool in_place = d->last.p && d->last.p == d->h0.p;   // its chunks would read what the last one writes
-  if (sh.W == SCAN_WAVES && rounds >= 4 && a.tiles < cus && !in_place) sh.K = std::min((2 * cus - 1) / a.tiles + 1, rounds);
+  if (sh.W == SCAN_WAVES && rounds >= 4 && d->T >= AUV_SCAN_SPLIT_STEPS && a.tiles < cus && !in_place)
+    sh.K = std::min((2 * cus - 1) / a.tiles + 1, rounds);
   a.chunk = ((rounds - 1) / sh.K + 1) * span;
   sh.K = (d->T - 1) / a.chunk + 1;
   a.K = sh.K;

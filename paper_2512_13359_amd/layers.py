@@ -35,21 +35,23 @@ def _one_of(fn, what, choices, v):
     return choices[v]
 
 
-def _like(fn, name, t, shape, dtype, device, contiguous=False):
-    """Checks a tensor."""
-    if t.dtype != dtype or t.shape != shape:
+def _like(fn, name, t, shape, dtype, index, contiguous=False):
+    """Checks a tensor; index: its device's."""
+    if t.dtype is dtype and t.shape == shape and t.get_device() == index and (not contiguous or t.is_contiguous()):
+        return
+    if t.dtype is not dtype or t.shape != shape:
         _refuse(fn, f"{name} must be {dtype} of shape {tuple(shape)}, got {t.dtype} of {tuple(t.shape)}")
-    if t.device != device:
-        _refuse(fn, f"{name} is on {t.device}, x on {device}")
-    if contiguous and not t.is_contiguous():
-        _refuse(fn, f"{name} must be contiguous")
+    if t.get_device() != index:
+        _refuse(fn, f"{name} is on another device than x: {t.device}")
+    _refuse(fn, f"{name} must be contiguous")
 
 
 def _here(fn, x, stream) -> bool:
     """Whether x's device is the current one and the stream its current stream."""
-    if not x.is_cuda:
+    index = x.get_device()
+    if index < 0:
         _refuse(fn, f"tensors must be on a GPU, x is on {x.device}")
-    return stream is None and x.get_device() == torch.cuda.current_device()
+    return stream is None and index == torch.cuda.current_device()
 
 
 def _packed(fn, kind, layout, *words):
@@ -82,7 +84,7 @@ def _work(n: int, x) -> torch.Tensor | None:
 
 def _scan(fn, gate, x, kind, done, lens, h0):
     """The structure's first words and its inputs' addresses and strides."""
-    shape, dtype, dev = x.shape, x.dtype, x.device
+    shape, dtype, dev = x.shape, x.dtype, x.get_device()
     if len(shape) != 3 or dtype not in TYPES:
         _refuse(fn, f"x must be a float32 or bfloat16 tensor [T][n][c], got {dtype} of {tuple(shape)}")
     T, n, c = shape
@@ -118,14 +120,14 @@ def scan_forward(gate, x, *, kind="sigmoid", done=None, lens=None, h0=None, out=
     fn = "scan_forward"
     head = _scan(fn, gate, x, kind, done, lens, h0)
     if out is not None:
-        _like(fn, "out", out, x.shape, x.dtype, x.device)
+        _like(fn, "out", out, x.shape, x.dtype, x.get_device())
     if not _here(fn, x, stream):
         with _Moved(x, stream):
             return scan_forward(gate, x, kind=kind, done=done, lens=lens, h0=h0, out=out)
     h = torch.empty_like(x) if out is None else out
     last = torch.empty(x.shape[1:], dtype=torch.float32, device=x.device) if h0 is None else torch.empty_like(h0)
     d = _packed(fn, A.AuvScan, _SCAN, *head, *_at(h), *_masks(done, lens, h0), *_at(last))
-    A.auv_scan_forward(d, _work(A.auv_scan_work_bytes(d), x))
+    A.auv_scan_forward(d, _work(A.auv_scan_work_bytes(d) if x.shape[0] >= A.AUV_SCAN_SPLIT_STEPS else 0, x))
     return h, last
 
 
@@ -137,16 +139,16 @@ def scan_backward(gate, x, h, *, dout=None, dh_last=None, kind="sigmoid", done=N
     buffer, say, where gate and x are the halves of one projection.  dh0 is float32 [n][c]."""
     fn = "scan_backward"
     head = _scan(fn, gate, x, kind, done, lens, h0)
-    _like(fn, "h", h, x.shape, x.dtype, x.device)
+    _like(fn, "h", h, x.shape, x.dtype, x.get_device())
     if dout is not None:
-        _like(fn, "dout", dout, x.shape, x.dtype, x.device)
+        _like(fn, "dout", dout, x.shape, x.dtype, x.get_device())
     if dh_last is not None:
-        _like(fn, "dh_last", dh_last, x.shape[1:], torch.float32, x.device)
+        _like(fn, "dh_last", dh_last, x.shape[1:], torch.float32, x.get_device())
     if out is not None:
         if len(out) != 2:
             _refuse(fn, "out must be the pair (dgate, dx)")
         for o in out:
-            _like(fn, "out", o, x.shape, x.dtype, x.device)
+            _like(fn, "out", o, x.shape, x.dtype, x.get_device())
     if not _here(fn, x, stream):
         with _Moved(x, stream):
             return scan_backward(gate, x, h, dout=dout, dh_last=dh_last, kind=kind, done=done, lens=lens, h0=h0, out=out)
@@ -156,7 +158,7 @@ def scan_backward(gate, x, h, *, dout=None, dh_last=None, kind="sigmoid", done=N
     d = _packed(fn, A.AuvScan, _SCAN, *head, *_at(h), *_masks(done, lens, h0), *_NONE)
     g = _packed(fn, A.AuvScanGrad, _SCAN_GRAD, *(_at(dout) if dout is not None else (0, 0, 0, 0)), *_at(dh_last), *_at(dgate),
                 *_at(dx), *_at(dh0))
-    A.auv_scan_backward(d, g, _work(A.auv_scan_work_bytes(d, g), x))
+    A.auv_scan_backward(d, g, _work(A.auv_scan_work_bytes(d, g) if x.shape[0] >= A.AUV_SCAN_SPLIT_STEPS else 0, x))
     return dgate, dx, dh0
 
 
@@ -190,9 +192,9 @@ def dropout(x, drop, add=None, *, out=None, stream=None):
     fn = "dropout"
     n, s, c = _sizes(fn, x)
     if add is not None:
-        _like(fn, "add", add, x.shape, x.dtype, x.device)
+        _like(fn, "add", add, x.shape, x.dtype, x.get_device())
     if out is not None:
-        _like(fn, "out", out, x.shape, x.dtype, x.device)
+        _like(fn, "out", out, x.shape, x.dtype, x.get_device())
     if not _here(fn, x, stream):
         with _Moved(x, stream):
             return dropout(x, drop, add, out=out)
@@ -206,9 +208,9 @@ def _norm(fn, x, groups, weight, bias, eps, act, drop):
     """The structure without mean and rstd; the callers hold `drop` while it is in use."""
     n, s, c = _sizes(fn, x)
     if weight is not None:
-        _like(fn, "weight", weight, (c,), torch.float32, x.device, True)
+        _like(fn, "weight", weight, (c,), torch.float32, x.get_device(), True)
     if bias is not None:
-        _like(fn, "bias", bias, (c,), torch.float32, x.device, True)
+        _like(fn, "bias", bias, (c,), torch.float32, x.get_device(), True)
     return _packed(fn, A.AuvNorm, _NORM, n, s, c, groups, TYPES[x.dtype], _one_of(fn, "act", ACTS, act), eps, *_rows(fn, "x", x),
                    0 if weight is None else weight.data_ptr(), 0 if bias is None else bias.data_ptr(), 0, 0,
                    0 if drop is None else A.address(drop))
@@ -225,7 +227,7 @@ def norm_forward(x, groups, *, weight=None, bias=None, eps=1e-5, act="none", dro
     fn = "norm_forward"
     d = _norm(fn, x, groups, weight, bias, eps, act, drop)
     if out is not None:
-        _like(fn, "out", out, x.shape, x.dtype, x.device)
+        _like(fn, "out", out, x.shape, x.dtype, x.get_device())
     if not _here(fn, x, stream):
         with _Moved(x, stream):
             return norm_forward(x, groups, weight=weight, bias=bias, eps=eps, act=act, drop=drop, out=out)
@@ -245,11 +247,11 @@ def norm_backward(x, groups, mean, rstd, dout, *, weight=None, bias=None, act="n
     fn = "norm_backward"
     d = _norm(fn, x, groups, weight, bias, 0.0, act, drop)
     for name, t in (("mean", mean), ("rstd", rstd)):
-        _like(fn, name, t, (d.n, groups), torch.float32, x.device, True)
+        _like(fn, name, t, (d.n, groups), torch.float32, x.get_device(), True)
     d.mean, d.rstd = mean.data_ptr(), rstd.data_ptr()
-    _like(fn, "dout", dout, x.shape, x.dtype, x.device)
+    _like(fn, "dout", dout, x.shape, x.dtype, x.get_device())
     if out is not None:
-        _like(fn, "out", out, x.shape, x.dtype, x.device)
+        _like(fn, "out", out, x.shape, x.dtype, x.get_device())
     if not _here(fn, x, stream):
         with _Moved(x, stream):
             return norm_backward(x, groups, mean, rstd, dout, weight=weight, bias=bias, act=act, drop=drop, out=out)

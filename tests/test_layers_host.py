@@ -51,6 +51,14 @@ def test_scan_workspace():
     assert A.auv_scan_work_bytes(long) > 0 and A.auv_scan_work_bytes(long, _grad(A)) > 0
     assert A.lib.auv_scan_forward(long, None, None) == A.AUV_EINVAL and "work" in A.auv_last_error()
     assert A.lib.auv_scan_backward(long, _grad(A), None, None) == A.AUV_EINVAL and "work" in A.auv_last_error()
+    # and never below the steps that the header names
+    for n, c in ((1, 1), (3, 8), (64, 64), (1, 5000)):
+        few = dict(T=A.AUV_SCAN_SPLIT_STEPS - 1, n=n, c=c)
+        few |= {f"{t}_{k}": v for t in ("gate", "x", "h") for k, v in (("st", n * c), ("sn", c))}
+        grad = {f"{t}_{k}": v for t in ("dout", "dgate", "dx") for k, v in (("st", n * c), ("sn", c))}
+        for typ in (A.AUV_FP32, A.AUV_BF16):
+            assert A.auv_scan_work_bytes(_scan(A, type=typ, **few)) == 0
+            assert A.auv_scan_work_bytes(_scan(A, type=typ, **few), _grad(A, **grad)) == 0
     # with the state updated in place the steps are not split: no chunk may read what the last one writes
     assert A.auv_scan_work_bytes(_scan(A, T=100000, h0=7 * P, h0_sn=8, h0_sc=1, last=7 * P, last_sn=8, last_sc=1)) == 0
     with pytest.raises(A.AuvError):
