@@ -490,8 +490,10 @@ enum { AUV_FP32 = 0, AUV_BF16 = 1 };
  *   s_t = 0 where the episode ended at step t (done nonzero), else h_t
  * Steps from a sequence's length on hold the state, h_t = s_t = s_{t-1}: their gate, input and
  * done are not looked at.  Nothing before an episode's end reaches what is after it, also not as
- * NaN.  The tensors may lie in any order ([T][n][c], [n][T][c], [c][T][n], parts of a wider
- * buffer, broadcast inputs); they run fastest where c or n is the axis of stride 1 in all. */
+ * NaN.  Steps are joined in ranges by the product of their f: decays above 1 whose product over some
+ * run of steps is beyond fp32 are right only where they meet a state (backward: a gradient) of zero.
+ * The tensors may lie in any order ([T][n][c], [n][T][c], [c][T][n], parts of a wider buffer,
+ * broadcast inputs); they run fastest where c or n is the axis of stride 1 in all. */
 enum { AUV_SCAN_SIGMOID = 0, AUV_SCAN_DECAY = 1 };
 
 typedef struct {

@@ -9,7 +9,8 @@
 // leaves in the caller's workspace.
 //
 // P = 0 stands for a cut (an episode's end) and nothing else: what was before a cut must not reach
-// what is after it, be it NaN or infinite.  A product that underflows keeps the smallest denormal.
+// what is after it, be it NaN or infinite.  A product that underflows keeps the smallest denormal.  P is kept finite: a
+// cut stays one beside any gates, and a state of zero gives S, in which gates that are not finite show as NaN.
 #pragma once
 
 #include "auv_internal.hpp"
@@ -44,9 +45,12 @@ struct ScanArgs {
 
 __device__ __forceinline__ float smallest() { return __uint_as_float(1u); }
 
+// NaN and infinities as the largest numbers
+__device__ __forceinline__ float finite(float P) { return fminf(fmaxf(P, -3.402823466e38f), 3.402823466e38f); }
+
 // P2 P1 where zero stands for a cut only
 __device__ __forceinline__ float chain(float P2, float P1) {
-  const float p = P2 * P1;
+  const float p = finite(P2 * P1);
   return p == 0.0f && P2 != 0.0f && P1 != 0.0f ? smallest() : p;
 }
 __device__ __forceinline__ float after(float P, float S, float s) { return P == 0.0f ? S : __builtin_fmaf(P, s, S); }
@@ -179,10 +183,10 @@ template <int V> __device__ __forceinline__ void join_range(const float* p, int 
     P[k] = chain(p2, P[k]);
   }
 }
-// The P of a wave's own steps: zero where a cut lies in them, never by underflow
+// The P of a wave's own steps: finite, zero where a cut lies in them, never by underflow
 template <int V> __device__ __forceinline__ void mark_cut(float* P, uint32_t cut) {
 #pragma unroll
-  for (int k = 0; k < V; ++k) P[k] = cut >> k & 1u ? 0.0f : (P[k] == 0.0f ? smallest() : P[k]);
+  for (int k = 0; k < V; ++k) P[k] = cut >> k & 1u ? 0.0f : (P[k] == 0.0f ? smallest() : finite(P[k]));
 }
 
 // Steps per wave and round, and the most waves of a workgroup (256 registers a lane)

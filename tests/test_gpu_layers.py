@@ -208,6 +208,62 @@ def test_scan_extreme_gates():
     assert torch.isinf(h).all() and torch.isinf(last).all()
 
 
+@pytest.mark.parametrize("T", [60, 400, 1500])
+@pytest.mark.parametrize("kind", ["sigmoid", "decay"])
+@pytest.mark.parametrize("typ", ["fp32", "bf16"])
+@pytest.mark.parametrize("bad", ["nan", "inf"])
+def test_scan_gates_that_are_not_finite_end_with_their_episode(bad, typ, kind, T):
+    """A gate that is NaN or infinite before an episode's end, in the same range of steps or an earlier one,
+    changes nothing after it, and one after the end changes no gradient up to it."""
+    require_gpu()
+    from paper_2512_13359_amd import scan_backward, scan_forward
+    n, c = 3, 8
+    gate, x, _, _, h0, dout, dlast = scan_inputs(T, n, c, typ, kind, "tnc", "h", 6)
+    for end in (T // 3, T // 2, 2 * T // 3):
+        done = torch.zeros(T, n, device="cuda")
+        done[end, 1] = 1.0
+        more = dict(kind=kind, done=done, h0=h0)
+        h, last = scan_forward(gate, x, **more)
+        clean = scan_backward(gate, x, h, dout=dout, dh_last=dlast, **more)
+        for at in {max(end - k, 0) for k in (0, 1, 9, 40, 70, 150, T)}:
+            dirty = gate.clone()
+            dirty[at, 1] = float(bad)
+            h2, last2 = scan_forward(dirty, x, **more)
+            assert torch.equal(last, last2) and torch.equal(h[end + 1:], h2[end + 1:]) and torch.equal(h[:, ::2], h2[:, ::2])
+        for at in {min(end + k, T - 1) for k in (1, 9, 40, 70, 150, T)}:
+            dirty = gate.clone()
+            dirty[at, 1] = float(bad)
+            got = scan_backward(dirty, x, h, dout=dout, dh_last=dlast, **more)
+            for p, q in zip(clean[:2], got[:2]):
+                assert torch.equal(p[:end + 1], q[:end + 1]) and torch.equal(p[:, ::2], q[:, ::2])
+            assert torch.equal(clean[2], got[2])
+
+
+@pytest.mark.parametrize("T", [200, 1500])
+@pytest.mark.parametrize("typ", ["fp32", "bf16"])
+def test_scan_large_decays_of_an_empty_state(typ, T):
+    """Decays whose product over many steps is beyond fp32 while the state, or the gradient, is zero: it stays zero."""
+    require_gpu()
+    from paper_2512_13359_amd import scan_backward, scan_forward
+    n, c, lo, hi = 2, 8, T // 4, 3 * T // 4
+    gate, x, _, _, _, dout, _ = scan_inputs(T, n, c, typ, "decay", "tnc", "", 7)
+    gate.fill_(0.5)
+    gate[lo:hi] = 100.0
+    x[:hi] = 0.0
+    dout[lo:] = 0.0
+    h, last = scan_forward(gate, x, kind="decay")
+    delta = np.full(x.shape, 24 * U)
+    wh, wl, bh, bl = L.scan(f64(gate), f64(x), kind="decay", delta=delta)
+    r = HALF[typ]
+    within(h, wh, bh + r * (np.abs(wh) + bh), "h")
+    within(last, wl, bl + U * np.abs(wl), "last")
+    dgate, dx, dh0 = scan_backward(gate, x, h, dout=dout, kind="decay")
+    wg, wx, w0, bg, bx, b0 = L.scan_grad(f64(gate), f64(x), f64(h), f64(dout), None, kind="decay", delta=delta)
+    within(dgate, wg, bg + r * (np.abs(wg) + bg), "dgate")
+    within(dx, wx, bx + r * (np.abs(wx) + bx), "dx")
+    within(dh0, w0, b0 + U * np.abs(w0), "dh0")
+
+
 def test_scan_broadcast_inputs_and_absent_gradients():
     """One decay for all sequences and steps (strides of zero); dout or dh_last absent stands for zero."""
     require_gpu()
