@@ -475,7 +475,7 @@ int auv_shac_window(auv_env* env, const auv_shac_config* cfg, const auv_mlp* pol
  * over the steps of a rollout (a memory for what one observation does not show, cut where
  * episodes end), group norm with an activation (one group and one position: layer norm), and
  * dropout from the counter-based generator.  Each has its gradient.  Tensors are fp32 or bf16
- * with strides in elements; sums, statistics and states are fp32, and a stored bf16 value is
+ * with strides in elements; sums, statistics and states are fp32 in both directions, and a stored bf16 value is
  * rounded once.  Sizes are >= 1.  Results are deterministic (same inputs, same bits).  Apart from what
  * a function names, its outputs share no memory with its inputs or each other; halves of one wider
  * buffer are separate tensors.  Pointers are aligned to their elements, `work` to 16 bytes.
@@ -510,7 +510,8 @@ typedef struct {
   int32_t T, n, c;      /* n c <= 2^30 */
   int32_t type, kind;   /* AUV_FP32 or AUV_BF16; AUV_SCAN_* */
   auv_seq gate, x;      /* inputs */
-  auv_seq h;            /* output of the forward pass, input of the backward pass */
+  auv_seq h;            /* output of the forward pass; input of the backward pass, which for bf16 forms the states again in
+                           fp32 from gate, x, done, lens and h0 instead of taking them from there */
   const float* done;    /* [T][n] as auv_rollout records it, or NULL */
   const int32_t* lens;  /* [n] steps of each sequence, below 0 as 0, above T as T; or NULL */
   auv_seq_state h0;     /* p NULL: zero */
@@ -524,9 +525,9 @@ typedef struct {
   auv_seq_state dh0;    /* result, or p NULL */
 } auv_scan_grad;
 
-/* Bytes of device workspace of auv_scan_forward (g NULL) or auv_scan_backward on these tensors:
- * 0 unless the columns are too few for the chip and the steps AUV_SCAN_SPLIT_STEPS at least (work may
- * then be NULL); -1 on bad arguments. */
+/* Bytes of device workspace of auv_scan_forward (g NULL) or auv_scan_backward on these tensors; -1 on bad
+ * arguments.  0 below AUV_SCAN_SPLIT_STEPS steps (work may then be NULL), and where the columns fill the chip but for a
+ * bf16 backward pass, which keeps the state before every 8 steps or more. */
 #define AUV_SCAN_SPLIT_STEPS 128
 int64_t auv_scan_work_bytes(const auv_scan* s, const auv_scan_grad* g);
 int auv_scan_forward(const auv_scan* s, void* work, void* stream);

@@ -53,12 +53,14 @@ def scan(gate, x, kind="sigmoid", done=None, lens=None, h0=None, delta=0.0):
 
 
 def scan_grad(gate, x, h, dout=None, dlast=None, kind="sigmoid", done=None, lens=None, h0=None, delta=0.0):
-    """(dgate, dx, dh0) and bounds on their rounding errors."""
-    gate, x, h = (np.asarray(v, np.float64) for v in (gate, x, h))
+    """(dgate, dx, dh0) and bounds on their rounding errors.  The state before a step is the recurrence's own, in 64 bits:
+    `h`, the output as it was stored, is rounded to the tensors' type and not looked at."""
+    gate, x = (np.asarray(v, np.float64) for v in (gate, x))
     T, n, c = x.shape
     f, w = _gates(gate, kind)
     end, hold = _masks(T, n, done, lens)
     delta = np.broadcast_to(np.asarray(delta, np.float64), x.shape)
+    state, _, es, _ = scan(gate, x, kind, done, lens, h0, delta)
     dout = np.zeros_like(x) if dout is None else np.asarray(dout, np.float64)
     G = np.zeros((n, c)) if dlast is None else np.array(dlast, np.float64)
     err = np.zeros((n, c))
@@ -68,16 +70,16 @@ def scan_grad(gate, x, h, dout=None, dlast=None, kind="sigmoid", done=None, lens
         g = dout[t] + G
         e = err + delta[t] * (np.abs(dout[t]) + np.abs(G))
         if t:
-            s = np.where(end[t - 1], 0.0, h[t - 1])
+            s, b = np.where(end[t - 1], 0.0, state[t - 1]), np.where(end[t - 1], 0.0, es[t - 1])
         else:
-            s = np.zeros((n, c)) if h0 is None else np.asarray(h0, np.float64)
+            s, b = np.zeros((n, c)) if h0 is None else np.asarray(h0, np.float64), np.zeros((n, c))
         if kind == "sigmoid":
             d = s - x[t]
             gz, gx = f[t] * w[t] * d * g, w[t] * g
-            ez = np.abs(f[t] * w[t]) * (np.abs(d) * e + 4 * delta[t] * (np.abs(s) + np.abs(x[t])) * np.abs(g))
+            ez = np.abs(f[t] * w[t]) * ((np.abs(d) + b) * e + (b + 4 * delta[t] * (np.abs(s) + np.abs(x[t]))) * np.abs(g))
             ew = np.abs(w[t]) * (e + delta[t] * np.abs(g))
         else:
-            gz, gx, ez, ew = s * g, g, np.abs(s) * (e + delta[t] * np.abs(g)), e
+            gz, gx, ez, ew = s * g, g, (np.abs(s) + b) * e + (b + np.abs(s) * delta[t]) * np.abs(g), e
         dgate[t], dx[t] = np.where(hold[t], 0.0, gz), np.where(hold[t], 0.0, gx)
         eg[t], ex[t] = np.where(hold[t], 0.0, ez), np.where(hold[t], 0.0, ew)
         G = np.where(hold[t], g, f[t] * g)

@@ -9,68 +9,6 @@
 
 namespace auv {
 
-// f and the input's share of U steps from t0 on; steps from tend on hold the state
-template <class T, int V, int U, bool SIG, bool MASK, bool NI>
-struct ForwardSteps {
-  Vec<T, V> z[U], x[U];
-  typename Columns<V, NI>::Flags d[MASK ? U : 1];
-
-  __device__ __forceinline__ void load(const ScanArgs& a, const Columns<V, NI>& col, const T* gate, const T* in, int t0,
-                                       int tend) {
-    const T *pz = gate + t0 * a.gate.st, *px = in + t0 * a.x.st;
-#pragma unroll
-    for (int u = 0; u < U; ++u, pz += a.gate.st, px += a.x.st) {
-      if (t0 + u < tend) {
-        z[u].load(pz);
-        x[u].load(px);
-        if constexpr (MASK)
-          if (a.done) d[u] = col.load_done(a, t0 + u);
-      }
-    }
-  }
-  __device__ __forceinline__ void masks(const ScanArgs& a, const Columns<V, NI>& col,
-                                        const typename Columns<V, NI>::Lens& len, int u, int t, uint32_t& done,
-                                        uint32_t& hold) const {
-    hold = col.over(len, t);
-    done = a.done ? col.ended(d[u]) & ~hold : 0u;
-  }
-  // f and the input's share of one step
-  __device__ __forceinline__ void step(int u, uint32_t hold, float* f, float* in) const {
-#pragma unroll
-    for (int k = 0; k < V; ++k) {
-      const float zz = z[u].get(k), xx = x[u].get(k);
-      if constexpr (SIG) {
-        float g;
-        sigmoid2<T>(zz, f[k], g);
-        in[k] = g * xx;
-      } else {
-        f[k] = zz;
-        in[k] = xx;
-      }
-    }
-    if (MASK && any_lane(hold)) {
-#pragma unroll
-      for (int k = 0; k < V; ++k)
-        if (hold >> k & 1u) f[k] = 1.0f, in[k] = 0.0f;
-    }
-  }
-};
-
-// One more step of a range's (P, S)
-template <bool MASK, int V>
-__device__ __forceinline__ void append(float* P, float* S, const float* f, const float* in, uint32_t done) {
-#pragma unroll
-  for (int k = 0; k < V; ++k) {
-    P[k] *= f[k];
-    S[k] = __builtin_fmaf(f[k], S[k], in[k]);
-  }
-  if (MASK && any_lane(done)) {
-#pragma unroll
-    for (int k = 0; k < V; ++k)
-      if (done >> k & 1u) P[k] = 1.0f, S[k] = 0.0f;
-  }
-}
-
 // (P, S) of every chunk of steps but the last: each wave runs a contiguous part of its chunk, the
 // first wave joins the parts.  Reads gate and input once: 2 x 256 bf16 columns x 32768 steps in 13 us (5.2 TB/s).
 template <class T, int V, bool SIG, bool MASK, bool NI>
@@ -212,15 +150,21 @@ __global__ __launch_bounds__(64 * SCAN_WAVES) void k_scan_forward(ScanArgs a) {
   }
 }
 
+int launch_scan_ranges(const char* fn, const ScanArgs& a, const ScanShape& sh, bool bf16, bool sig, hipStream_t s) {
+  const bool mask = a.done || a.lens;
+  ScanArgs arg = a;
+  void* args[1] = {&arg};
+  return launch_kernel(fn, AUV_SCAN_KERNEL(k_scan_ranges), dim3(a.tiles * (sh.K - 1)), dim3(64 * sh.W), args,
+                       sh.W * sizeof(float) * 128 * sh.V, s);
+}
+
 int launch_scan_forward(const ScanArgs& a, const ScanShape& sh, bool bf16, bool sig, hipStream_t s) {
   const bool mask = a.done || a.lens;
   ScanArgs arg = a;
   void* args[1] = {&arg};
   const size_t range = sizeof(float) * 128 * sh.V;
   if (sh.K > 1)
-    if (int rc = launch_kernel("auv_scan_forward", AUV_SCAN_KERNEL(k_scan_ranges), dim3(a.tiles * (sh.K - 1)), dim3(64 * sh.W), args,
-                               sh.W * range, s))
-      return rc;
+    if (int rc = launch_scan_ranges("auv_scan_forward", a, sh, bf16, sig, s)) return rc;
   return launch_kernel("auv_scan_forward", AUV_SCAN_KERNEL(k_scan_forward), dim3(a.tiles * sh.K), dim3(64 * sh.W), args,
                        2 * sh.W * range, s);
 }
@@ -310,12 +254,16 @@ static void scan_shape(const auv_scan* d, const auv_seq* const* seqs, int count,
   if (sh.V == 2 && d->type == AUV_FP32 && tiles_of(2) < cus && tiles_of(1) >= cus) sh.V = 1;
   a.nvec = (a.Li + sh.V - 1) / sh.V;
   a.tiles = tiles_of(sh.V);
-  const int U = sh.V >= (grad ? 2 : 4) ? 4 : 8;   // scan_steps, scan_grad_steps
+  const int U = sh.steps = sh.V >= (grad ? 2 : 4) ? 4 : 8;   // scan_steps, scan_grad_steps
   // Waves per workgroup until there are eight per CU (4095 x 23 fp32 columns x 500 steps, 736 tiles, forward and backward: one wave
   // 160 and 355 us, two 145 and 260, four 142 and 243; where there are eight anyway one wave is best, 16384 x 64 columns x 64 steps: 81, two
   // waves 88); four per CU do for accesses of 16 bytes (4096 x 64 fp32 columns x 128: one wave 73 and 149, two 79 and 157).
+  // A bf16 gradient leaves the state before each round: rounds of 8 steps at least (a quarter of a tensor in the workspace, or
+  // 16 KB of LDS; backward of 16384 x 64 columns x 64 steps: 4 steps 215 us, 8 187, 16 194; 4096 x 64 x 512: 8 411, 16 495).
   sh.W = 1;
-  while (sh.W < SCAN_WAVES && (int64_t)a.tiles * sh.W < (sh.V == 4 && d->type == AUV_FP32 ? 4 : 8) * cus && sh.W * U < d->T) sh.W *= 2;
+  const bool marks = grad && d->type == AUV_BF16;
+  const int enough = sh.V == 4 && d->type == AUV_FP32 ? 4 : 8;
+  while (sh.W < SCAN_WAVES && sh.W * U < d->T && ((int64_t)a.tiles * sh.W < enough * cus || (marks && sh.W * U < 8))) sh.W *= 2;
   const int span = sh.W * U, rounds = (d->T - 1) / span + 1;
   // Steps split over workgroups where there is less than one per CU, up to two per CU: reads gate and input (or dout) twice.
   // 2048 columns x 4096 steps: whole 201 and 398 us, split in 16 30 and 43, in 32 25 and 33; 16384 columns x 1024 steps: whole 54 and
@@ -359,8 +307,15 @@ static void backward_args(const auv_scan* d, const auv_scan_grad* g, ScanArgs& a
   a.dx = inner_first(g->dx, sh.ni);
 }
 
-static int64_t ranges_bytes(const ScanArgs& a, const ScanShape& sh) {
-  return sh.K > 1 ? (int64_t)sh.K * a.tiles * 128 * sh.V * sizeof(float) : 0;
+// A call's workspace: the ranges of split steps, a bf16 gradient's in both directions, and its states before the rounds.
+static int64_t place_work(const auv_scan* d, const auv_scan_grad* g, ScanArgs& a, const ScanShape& sh, void* work) {
+  const bool form = g && d->type == AUV_BF16;
+  const int64_t range = sh.K > 1 ? (int64_t)sh.K * a.tiles * 128 * sh.V : 0;   // floats
+  const int64_t marks = form && d->T >= AUV_SCAN_SPLIT_STEPS ? (int64_t)sh.K * (a.chunk / (sh.W * sh.steps)) * a.tiles * 64 * sh.V : 0;
+  a.agg = static_cast<float*>(work);
+  a.before = work && form ? a.agg + range : nullptr;
+  a.marks = work && marks ? a.agg + 2 * range : nullptr;
+  return (range * (form ? 2 : 1) + marks) * (int64_t)sizeof(float);
 }
 
 }  // namespace auv
@@ -376,7 +331,7 @@ int64_t auv_scan_work_bytes(const auv_scan* d, const auv_scan_grad* g) {
   ScanShape sh{};
   if (g) backward_args(d, g, a, sh);
   else forward_args(d, a, sh);
-  return ranges_bytes(a, sh);
+  return place_work(d, g, a, sh, nullptr);
 }
 
 int auv_scan_forward(const auv_scan* d, void* work, void* stream) {
@@ -393,10 +348,10 @@ int auv_scan_forward(const auv_scan* d, void* work, void* stream) {
   ScanArgs a{};
   ScanShape sh{};
   forward_args(d, a, sh);
-  if (sh.K > 1 && (!work || !aligned16(work))) return set_error(AUV_EINVAL, "%s: 'work' is NULL or not 16-byte aligned", fn);
+  if (place_work(d, nullptr, a, sh, work) && (!work || !aligned16(work)))
+    return set_error(AUV_EINVAL, "%s: 'work' is NULL or not 16-byte aligned", fn);
   a.h0 = {d->h0.p, d->h0.sn, d->h0.sc};
   a.last = {d->last.p, d->last.sn, d->last.sc};
-  a.agg = static_cast<float*>(work);
   return launch_scan_forward(a, sh, d->type == AUV_BF16, d->kind == AUV_SCAN_SIGMOID, (hipStream_t)stream);
 }
 
@@ -423,11 +378,11 @@ int auv_scan_backward(const auv_scan* d, const auv_scan_grad* g, void* work, voi
   ScanArgs a{};
   ScanShape sh{};
   backward_args(d, g, a, sh);
-  if (sh.K > 1 && (!work || !aligned16(work))) return set_error(AUV_EINVAL, "%s: 'work' is NULL or not 16-byte aligned", fn);
+  if (place_work(d, g, a, sh, work) && (!work || !aligned16(work)))
+    return set_error(AUV_EINVAL, "%s: 'work' is NULL or not 16-byte aligned", fn);
   a.h0 = {d->h0.p, d->h0.sn, d->h0.sc};
   a.last = {g->dlast.p, g->dlast.sn, g->dlast.sc};
   a.dh0 = {g->dh0.p, g->dh0.sn, g->dh0.sc};
-  a.agg = static_cast<float*>(work);
   return launch_scan_backward(a, sh, d->type == AUV_BF16, d->kind == AUV_SCAN_SIGMOID, (hipStream_t)stream);
 }
 

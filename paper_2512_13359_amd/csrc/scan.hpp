@@ -34,6 +34,8 @@ struct ScanArgs {
   const float* done;     // [T][n] or null
   const int32_t* lens;   // [n] or null
   float* agg;            // [K][tiles][V][2][64]
+  float* before;         // the same of the forward pass, for a gradient that forms the states again
+  float* marks;          // the state before each round, [K][rounds][tiles][V][64]; null: in LDS
   int T, n, c;
   int Li, Lo;            // columns as [Lo][Li]; Li is the axis of unit stride
   int nvec;              // vectors per row of Li
@@ -163,17 +165,20 @@ template <int V, bool NI> struct Columns {
   }
 };
 
-// (P, S) of V columns in LDS or in the workspace: [V][2][64], a lane's values 64 floats apart
-template <int V> __device__ __forceinline__ void put_range(float* p, int lane, const float* P, const float* S) {
+// (P, S) of V columns in LDS or in the workspace: [V][2][64], a lane's values 64 floats apart; with the S of both
+// directions [V][3][64], of which I = 1 or 2 is run
+template <int V, int N = 2> __device__ __forceinline__ void put_range(float* p, int lane, const float* P, const float* S,
+                                                                      const float* S2 = nullptr) {
 #pragma unroll
   for (int k = 0; k < V; ++k) {
-    p[(2 * k) * 64 + lane] = P[k];
-    p[(2 * k + 1) * 64 + lane] = S[k];
+    p[(N * k) * 64 + lane] = P[k];
+    p[(N * k + 1) * 64 + lane] = S[k];
+    if constexpr (N == 3) p[(N * k + 2) * 64 + lane] = S2[k];
   }
 }
-template <int V> __device__ __forceinline__ void run_range(const float* p, int lane, float* s) {
+template <int V, int N = 2, int I = 1> __device__ __forceinline__ void run_range(const float* p, int lane, float* s) {
 #pragma unroll
-  for (int k = 0; k < V; ++k) s[k] = after(p[(2 * k) * 64 + lane], p[(2 * k + 1) * 64 + lane], s[k]);
+  for (int k = 0; k < V; ++k) s[k] = after(p[(N * k) * 64 + lane], p[(N * k + I) * 64 + lane], s[k]);
 }
 template <int V> __device__ __forceinline__ void join_range(const float* p, int lane, float* P, float* S) {
 #pragma unroll
@@ -197,11 +202,74 @@ constexpr int SCAN_WAVES = 8;
 // Flags are rare: the selects for a step are jumped over where no lane of the wave has one.
 __device__ __forceinline__ bool any_lane(uint32_t bits) { return __ballot(bits != 0u) != 0ull; }
 
+// f and the input's share of U steps from t0 on; steps from tend on hold the state
+template <class T, int V, int U, bool SIG, bool MASK, bool NI>
+struct ForwardSteps {
+  Vec<T, V> z[U], x[U];
+  typename Columns<V, NI>::Flags d[MASK ? U : 1];
+
+  __device__ __forceinline__ void load(const ScanArgs& a, const Columns<V, NI>& col, const T* gate, const T* in, int t0,
+                                       int tend) {
+    const T *pz = gate + t0 * a.gate.st, *px = in + t0 * a.x.st;
+#pragma unroll
+    for (int u = 0; u < U; ++u, pz += a.gate.st, px += a.x.st) {
+      if (t0 + u < tend) {
+        z[u].load(pz);
+        x[u].load(px);
+        if constexpr (MASK)
+          if (a.done) d[u] = col.load_done(a, t0 + u);
+      }
+    }
+  }
+  __device__ __forceinline__ void masks(const ScanArgs& a, const Columns<V, NI>& col,
+                                        const typename Columns<V, NI>::Lens& len, int u, int t, uint32_t& done,
+                                        uint32_t& hold) const {
+    hold = col.over(len, t);
+    done = a.done ? col.ended(d[u]) & ~hold : 0u;
+  }
+  // f and the input's share of one step
+  __device__ __forceinline__ void step(int u, uint32_t hold, float* f, float* in) const {
+#pragma unroll
+    for (int k = 0; k < V; ++k) {
+      const float zz = z[u].get(k), xx = x[u].get(k);
+      if constexpr (SIG) {
+        float g;
+        sigmoid2<T>(zz, f[k], g);
+        in[k] = g * xx;
+      } else {
+        f[k] = zz;
+        in[k] = xx;
+      }
+    }
+    if (MASK && any_lane(hold)) {
+#pragma unroll
+      for (int k = 0; k < V; ++k)
+        if (hold >> k & 1u) f[k] = 1.0f, in[k] = 0.0f;
+    }
+  }
+};
+
+// One more step of a range's (P, S)
+template <bool MASK, int V>
+__device__ __forceinline__ void append(float* P, float* S, const float* f, const float* in, uint32_t done) {
+#pragma unroll
+  for (int k = 0; k < V; ++k) {
+    P[k] *= f[k];
+    S[k] = __builtin_fmaf(f[k], S[k], in[k]);
+  }
+  if (MASK && any_lane(done)) {
+#pragma unroll
+    for (int k = 0; k < V; ++k)
+      if (done >> k & 1u) P[k] = 1.0f, S[k] = 0.0f;
+  }
+}
+
 // launches implemented in scan.hip (shape and argument checks) and scan_backward.hip
 struct ScanShape {
-  int V, W, K;
+  int V, W, K, steps;   // steps: per wave and round
   bool ni;
 };
+int launch_scan_ranges(const char* fn, const ScanArgs& a, const ScanShape& sh, bool bf16, bool sig, hipStream_t s);   // forward, to a.agg
 int launch_scan_forward(const ScanArgs& a, const ScanShape& sh, bool bf16, bool sig, hipStream_t s);
 int launch_scan_backward(const ScanArgs& a, const ScanShape& sh, bool bf16, bool sig, hipStream_t s);
 

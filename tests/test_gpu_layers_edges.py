@@ -1,0 +1,94 @@
+"""More GPU parity of the network layers with their float64 oracle: states that follow their input, and other uses where an
+error hides behind random numbers.  Tolerances as derived in test_gpu_layers.py."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import layers as L
+from tests.gpu_util import announce, host, require_gpu
+from tests.test_gpu_layers import HALF, TYPES, U, f64, scan_inputs, seq, within
+
+pytestmark = pytest.mark.gpu
+
+
+def check_following_state(T, n, c, typ, kind, order, masks):
+    """x = 1 + 0.01 noise: the state lies next to its input, and dgate = f (1 - f) (s - x) g is their small difference.
+    dgate is compared with the gradient of the recurrence itself; a state rounded to bf16 would leave an error of 2^-9
+    beside differences of about 2^-7.  The oracle runs on a few sequences (they are independent)."""
+    from paper_2512_13359_amd import scan_backward, scan_forward
+    announce(f"scan following T={T} n={n} c={c} {typ} {kind} {order} '{masks}'")
+    _, _, done, lens, h0, _, dlast = scan_inputs(T, n, 1, typ, kind, "tnc", masks, T + c)
+    g = torch.Generator(device="cuda")
+    g.manual_seed(n)
+    gate, x, dout = seq(g, T, n, c, typ, order, 1.5, 2.2), seq(g, T, n, c, typ, order, 0.01, 1.0), seq(g, T, n, c, typ, order)
+    if kind == "decay":
+        gate.copy_(torch.sigmoid(gate.float()))
+    h0 = None if h0 is None else 1 + 0.01 * torch.randn(n, c, generator=g, device="cuda")
+    dlast = dlast.expand(n, c).contiguous()
+    more = dict(kind=kind, done=done, lens=lens, h0=h0)
+    h, _ = scan_forward(gate, x, **more)
+    dgate, dx, dh0 = scan_backward(gate, x, h, dout=dout, dh_last=dlast, **more)
+    some = sorted({*range(min(n, 4)), n // 2, *range(max(n - 3, 0), n)})
+    pick = lambda t, axis=1: None if t is None else f64(t.index_select(axis, torch.tensor(some, device="cuda")))  # noqa: E731
+    delta = (np.abs(pick(gate)) * (kind == "sigmoid") + 24) * U
+    m = dict(kind=kind, done=pick(done), lens=None if lens is None else host(lens)[some], h0=pick(h0, 0), delta=delta)
+    wg, wx, w0, bg, bx, b0 = L.scan_grad(pick(gate), pick(x), None, pick(dout), pick(dlast, 0), **m)
+    r = HALF[typ]
+    within(pick_f(dgate, some), wg, bg + r * (np.abs(wg) + bg), "dgate")
+    within(pick_f(dx, some), wx, bx + r * (np.abs(wx) + bx), "dx")
+    within(dh0[some], w0, b0 + U * np.abs(w0), "dh0")
+
+
+def pick_f(t, some):
+    return t.index_select(1, torch.tensor(some, device=t.device))
+
+
+@pytest.mark.parametrize("kind", ["sigmoid", "decay"])
+@pytest.mark.parametrize("typ", ["fp32", "bf16"])
+@pytest.mark.parametrize("T, n, c", [(1, 3, 5), (5, 40, 8), (16, 7, 24), (17, 7, 24), (100, 3, 70), (127, 33, 9), (128, 33, 9), (129, 33, 9),
+                                     (512, 6, 64), (4001, 2, 33), (700, 2049, 8), (9, 4100, 64), (127, 4100, 64), (150, 4100, 64), (40, 16500, 5)])
+def test_scan_gradient_of_states_that_follow_their_input(T, n, c, typ, kind):
+    """Every width of a lane's columns, one workgroup to many, the marks in LDS and in the workspace, split steps."""
+    require_gpu()
+    check_following_state(T, n, c, typ, kind, "tnc", "dl")
+
+
+@pytest.mark.parametrize("order", ["tnc", "ntc", "cnt", "nct", "tcn", "odd"])
+@pytest.mark.parametrize("masks", ["", "h", "d", "l"])
+def test_scan_gradient_of_following_states_by_order(order, masks):
+    require_gpu()
+    for T, n, c in ((37, 9, 6), (300, 70, 40), (2000, 3, 20)):
+        for kind in ("sigmoid", "decay"):
+            check_following_state(T, n, c, "bf16", kind, order, masks)
+
+
+def test_scan_gradient_captured_and_on_two_streams():
+    """A bf16 gradient's workspace is the call's own: two streams at once, a graph replayed with eager work between."""
+    require_gpu()
+    from paper_2512_13359_amd import scan_backward, scan_forward
+    T, n, c = 1500, 4, 40
+    gate, x, done, _, h0, dout, dlast = scan_inputs(T, n, c, "bf16", "sigmoid", "tnc", "d", 3)
+    other = scan_inputs(T, n, c, "bf16", "sigmoid", "tnc", "d", 4)[1]
+
+    def both(x, stream=None):
+        h, last = scan_forward(gate, x, done=done, h0=h0, stream=stream)
+        return (h, last, *scan_backward(gate, x, h, dout=dout, dh_last=dlast, done=done, h0=h0, stream=stream))
+
+    want = {False: both(x), True: both(other)}
+    assert not torch.equal(want[False][2], want[True][2])
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    outs = [both(other if k % 2 else x, streams[k % 2]) for k in range(6)]
+    torch.cuda.synchronize()
+    for k, out in enumerate(outs):
+        assert all(torch.equal(p, q) for p, q in zip(out, want[k % 2 == 1])), k
+    held = x.clone()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = both(held)
+    for rep in range(4):
+        held.copy_(other if rep % 2 else x)
+        graph.replay()
+        both(x)
+        torch.cuda.synchronize()
+        assert all(torch.equal(p, q) for p, q in zip(out, want[rep % 2 == 1])), rep
