@@ -315,8 +315,8 @@ __global__ __launch_bounds__(512) void k_norm_block_grad(NormArgs a) {
 
 // ------------------------------------------------------------------ chunk form -------
 // A workgroup walks over a chunk of a sample's positions and a tile of its channels, a thread keeping V channels.  The
-// first launch leaves every chunk's and tile's share of each group's statistics, [n][chunk][tile][G]; the second joins a
-// group's shares in its first instructions.  Bound by HBM and the second read: 32 x 4096 x 256 bf16 in 32 groups with SiLU, 13 us for the
+// first launch leaves every chunk's and tile's share of the statistics of the tile's groups, [n][chunk][tile][held]; the second
+// joins a group's shares in its first instructions.  Bound by HBM and the second read: 32 x 4096 x 256 bf16 in 32 groups with SiLU, 13 us for the
 // statistics (5.2 TB/s) and 26 for the rest (5.2); backward 68.
 template <class T, int V> struct Walker {
   bool on;
@@ -347,17 +347,18 @@ template <class T, int V> struct Walker {
     lo = max(g * a.Cg - base, 0);
     hi = min((g + 1) * a.Cg - base, local);
   }
-  __device__ __forceinline__ float2* share(const NormArgs& a) const {   // [G] of this chunk and tile
-    return reinterpret_cast<float2*>(a.groups) + (((int64_t)i * a.chunks + chunk) * a.tiles + blockIdx.y) * a.G;
+  __device__ __forceinline__ float2* share(const NormArgs& a) const {   // of this chunk and tile, from group g0 on
+    return reinterpret_cast<float2*>(a.groups) + (((int64_t)i * a.chunks + chunk) * a.tiles + blockIdx.y) * a.held;
   }
   // f(lane, lanes, share of group g by chunk and tile, its positions and channels) for all of them, dealt out to `lanes` lanes
   template <class F> __device__ __forceinline__ void shares_of(const NormArgs& a, int g, int lane, int lanes, F f) const {
     const int wide = a.tile * V, t0 = g * a.Cg / wide, t1 = (g * a.Cg + a.Cg - 1) / wide, nt = t1 - t0 + 1;
-    const float2* p = reinterpret_cast<const float2*>(a.groups) + ((int64_t)i * a.chunks * a.tiles + t0) * a.G + g;
+    const float2* p = reinterpret_cast<const float2*>(a.groups) + ((int64_t)i * a.chunks * a.tiles + t0) * a.held;
+    const int first = g - t0 * wide / a.Cg;   // its place in the tile it starts in; it is the first of the others
     for (int k = lane; k < a.chunks * nt; k += lanes) {
       const int ch = k / nt, t = k - ch * nt, c0 = (t0 + t) * wide;
       const int count = min((g + 1) * a.Cg, c0 + wide) - max(g * a.Cg, c0);
-      f(p[((int64_t)ch * a.tiles + t) * a.G], min(a.S, (ch + 1) * a.per) - ch * a.per, count);
+      f(p[((int64_t)ch * a.tiles + t) * a.held + (t ? 0 : first)], min(a.S, (ch + 1) * a.per) - ch * a.per, count);
     }
   }
   // whether this workgroup writes group g's statistics
@@ -483,7 +484,7 @@ __global__ __launch_bounds__(256) void k_norm_stats(NormArgs a) {
       M += __builtin_fmaf((float)(whole + (r < rest)) * d, d, squares[r * width + q]);
     }
     M = team_sum(M, lanes);
-    if (l == 0) wk.share(a)[g] = make_float2(mean, M);
+    if (l == 0) wk.share(a)[g - wk.g0] = make_float2(mean, M);
   }
 }
 
@@ -623,7 +624,7 @@ __global__ __launch_bounds__(256) void k_norm_grad_sums(NormArgs a) {
     }
     s1 = team_sum(s1, lanes);
     s2 = team_sum(s2, lanes);
-    if (l == 0) wk.share(a)[g] = make_float2(s1, s2);
+    if (l == 0) wk.share(a)[g - wk.g0] = make_float2(s1, s2);
   }
 }
 
@@ -816,12 +817,18 @@ static int plan(const char* fn, const auv_norm* d, bool dense, bool backward, No
   return plan_chunks(fn, d, p);
 }
 
+// groups that a tile of channels can hold a part of
+static int tile_groups(const auv_norm* d, const NormPlan& p) {
+  const int wide = std::min(p.tile * p.V, d->c), cg = d->c / d->groups;
+  return std::min(d->groups, (wide - 1) / cg + 2);
+}
+
 static int64_t part_floats(const NormPlan& p, int64_t c, bool backward) {
   return backward ? (p.part_rows * 2 * c + 3) / 4 * 4 : 0;
 }
 
 static int64_t plan_bytes(const auv_norm* d, const NormPlan& p, bool backward) {
-  const int64_t shares = p.form == NORM_CHUNKS ? (int64_t)d->n * p.chunks * p.tiles * d->groups * 2 : 0;
+  const int64_t shares = p.form == NORM_CHUNKS ? (int64_t)d->n * p.chunks * p.tiles * tile_groups(d, p) * 2 : 0;
   return (part_floats(p, d->c, backward) + shares) * (int64_t)sizeof(float);
 }
 
@@ -877,15 +884,10 @@ static NormArgs norm_args(const auv_norm* d, const NormPlan& p) {
   a.pack = p.pack;
   a.chunks = p.chunks;
   a.per = p.per;
+  a.held = p.form == NORM_CHUNKS ? tile_groups(d, p) : 0;
   a.part_rows = (int)p.part_rows;
   a.drop = drop_args(d->drop);
   return a;
-}
-
-// groups that a tile of channels can hold a part of
-static size_t tile_groups(const auv_norm* d, const NormPlan& p) {
-  const int wide = std::min(p.tile * p.V, d->c), cg = d->c / d->groups;
-  return std::min<size_t>(d->groups, (size_t)(wide - 1) / cg + 2);
 }
 
 }  // namespace auv
@@ -924,7 +926,7 @@ int auv_norm_forward(const auv_norm* d, const auv_rows* y, void* work, void* str
   const dim3 grid((unsigned)p.part_rows, p.tiles);
   const size_t lds = 2 * sizeof(float) * (256 / p.tile) * p.tile * p.V;
   if (int rc = launch_kernel(fn, AUV_CHUNK_KERNEL(k_norm_stats), grid, dim3(256), args, lds, s)) return rc;
-  return launch_kernel(fn, AUV_CHUNK_KERNEL(k_norm_apply), grid, dim3(256), args, 2 * sizeof(float) * tile_groups(d, p), s);
+  return launch_kernel(fn, AUV_CHUNK_KERNEL(k_norm_apply), grid, dim3(256), args, 2 * sizeof(float) * a.held, s);
 }
 
 int auv_norm_backward(const auv_norm* d, const auv_norm_grad* g, void* work, void* stream) {
@@ -965,7 +967,7 @@ int auv_norm_backward(const auv_norm* d, const auv_norm_grad* g, void* work, voi
     const size_t lds = 2 * sizeof(float) * (256 / p.tile) * p.tile * p.V;
     a.groups = a.part + part_floats(p, d->c, true);
     if (int rc = launch_kernel(fn, AUV_CHUNK_KERNEL(k_norm_grad_sums), grid, dim3(256), args, lds, s)) return rc;
-    if (int rc = launch_kernel(fn, AUV_CHUNK_KERNEL(k_norm_grad_apply), grid, dim3(256), args, 2 * sizeof(float) * tile_groups(d, p), s))
+    if (int rc = launch_kernel(fn, AUV_CHUNK_KERNEL(k_norm_grad_apply), grid, dim3(256), args, 2 * sizeof(float) * a.held, s))
       return rc;
   }
   if (!params) return AUV_OK;

@@ -16,7 +16,7 @@ struct NormArgs {
   const float *w, *b;
   float *mean, *rstd;
   float* part;    // backward: rows of partial sums of dw and db, [2][C] each
-  float* groups;  // chunk form: [n][chunk][tile][G][2] moments (forward) or sums of d and d xhat (backward)
+  float* groups;  // chunk form: [n][chunk][tile][held][2] moments (forward) or sums of d and d xhat (backward)
   float *dw, *db;
   float eps;
   int act, n, S, C, G, Cg;
@@ -24,6 +24,7 @@ struct NormArgs {
   int tile, tiles;   // vectors of a row per workgroup, workgroups across it
   int step, pack;    // block form: positions per pass, samples per pass
   int chunks, per;   // chunk form: chunks of `per` positions
+  int held;          // chunk form: groups that a tile can hold a part of
   int part_rows;
   DropArgs drop;
 };

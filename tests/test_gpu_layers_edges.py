@@ -6,7 +6,7 @@ import torch
 
 from oracle import layers as L
 from tests.gpu_util import announce, host, require_gpu
-from tests.test_gpu_layers import HALF, TYPES, U, f64, scan_inputs, seq, within
+from tests.test_gpu_layers import HALF, TYPES, U, check_norm, f64, scan_inputs, seq, within
 
 pytestmark = pytest.mark.gpu
 
@@ -92,3 +92,10 @@ def test_scan_gradient_captured_and_on_two_streams():
         both(x)
         torch.cuda.synchronize()
         assert all(torch.equal(p, q) for p, q in zip(out, want[rep % 2 == 1])), rep
+
+
+def test_norm_of_single_channels_in_wide_rows():
+    """As many groups as channels over several tiles: each tile has shares of its own groups."""
+    require_gpu()
+    check_norm(3, 40, 5000, 5000, "fp32", "tanh", seed=1)
+    check_norm(2, 300, 4500, 1500, "bf16", "relu", drop=9000, seed=2)
