@@ -551,38 +551,19 @@ __global__ __launch_bounds__(256) void k_norm_apply(NormArgs a) {
   });
 }
 
-template <class T, int V, bool DROP>
+// MANY: a workgroup takes every `slots`-th sample and keeps the sums of the parameters' gradients over them in registers, so that
+// 65536 rows of 8192 bf16 channels leave 256 partial rows (17 MB), not one each.
+template <class T, int V, bool DROP, bool MANY>
 __global__ __launch_bounds__(256) void k_norm_grad_sums(NormArgs a) {
   extern __shared__ float red[];   // [2][step][tile V], then sums in their first rows
-  const Walker<T, V> wk(a);
+  Walker<T, V> wk(a);
   const int width = a.tile * V;
   float *dws = red, *dbs = red + wk.step * width;
-  if (wk.on) {
-    const ChannelValues<V> ch(a, wk.c, 0);
-    float mean[V], rstd[V], dw[V], db[V];
+  float* out = a.part ? a.part + (int64_t)blockIdx.x * 2 * a.C + wk.base : nullptr;
+  float all_w[V], all_b[V];
 #pragma unroll
-    for (int k = 0; k < V; ++k) {
-      mean[k] = a.mean[(int64_t)wk.i * a.G + ch.g[k]];
-      rstd[k] = a.rstd[(int64_t)wk.i * a.G + ch.g[k]];
-      dw[k] = db[k] = 0.0f;
-    }
-    walk<T, V, 2, false>(wk, wk.in(a.x, a.x_sn), a.x_ss, wk.in(a.dout, a.dout_sn), a.dout_ss, [&](int s, const Vec<T, V>& q, const Vec<T, V>& e) {
-      float xh[V], du[V];
-      Draws<V> keep;
-      if constexpr (DROP) keep.draw(a.drop, (uint32_t)((int64_t)wk.i * a.S + s), wk.c);
-#pragma unroll
-      for (int k = 0; k < V; ++k) {
-        float v = q.get(k);
-        if constexpr (DROP) v = keep.kept(a.drop, k) ? v : 0.0f;
-        xh[k] = __builtin_fmaf(v, a.drop.scale, -mean[k]) * rstd[k];
-      }
-      grad_of<T, V>(a.act, ch.w, ch.b, e, xh, du);
-#pragma unroll
-      for (int k = 0; k < V; ++k) {
-        dw[k] = __builtin_fmaf(du[k], xh[k], dw[k]);
-        db[k] += du[k];
-      }
-    });
+  for (int k = 0; k < V; ++k) all_w[k] = all_b[k] = 0.0f;
+  auto put = [&](const float* dw, const float* db) {
     const int at = wk.row * width + wk.c - wk.base;
 #pragma unroll
     for (int k = 0; k < V; ++k)
@@ -590,42 +571,96 @@ __global__ __launch_bounds__(256) void k_norm_grad_sums(NormArgs a) {
         dws[at + k] = dw[k];
         dbs[at + k] = db[k];
       }
-  }
-  __syncthreads();
-  float* out = a.part + (int64_t)blockIdx.x * 2 * a.C + wk.base;
-  const int per = lanes_for(min(wk.step, wk.local >= 256 ? 1 : 256 / wk.local));   // lanes per channel
-  for (int t = threadIdx.x; t / per < wk.local; t += 256) {
-    const int q = t / per, l = t & (per - 1);
-    float dw = 0.0f, db = 0.0f;
-    for (int r = l; r < wk.step; r += per) {
-      dw += dws[r * width + q];
-      db += dbs[r * width + q];
+  };
+  // the rows' sums, f(channel of the tile, dw, db) for each by one lane
+  auto sum_rows = [&](auto f) {
+    const int per = lanes_for(min(wk.step, wk.local >= 256 ? 1 : 256 / wk.local));   // lanes per channel
+    for (int t = threadIdx.x; t / per < wk.local; t += 256) {
+      const int q = t / per, l = t & (per - 1);
+      float dw = 0.0f, db = 0.0f;
+      for (int r = l; r < wk.step; r += per) {
+        dw += dws[r * width + q];
+        db += dbs[r * width + q];
+      }
+      dw = team_sum(dw, per);
+      db = team_sum(db, per);
+      if (l == 0) f(q, dw, db);
     }
-    dw = team_sum(dw, per);
-    db = team_sum(db, per);
-    if (l == 0) {   // row 0 of a channel is this team's own
-      out[q] = dw;
-      out[a.C + q] = db;
+  };
+  for (;;) {
+    if (wk.on) {
+      const ChannelValues<V> ch(a, wk.c, 0);
+      float mean[V], rstd[V], dw[V], db[V];
+#pragma unroll
+      for (int k = 0; k < V; ++k) {
+        mean[k] = a.mean[(int64_t)wk.i * a.G + ch.g[k]];
+        rstd[k] = a.rstd[(int64_t)wk.i * a.G + ch.g[k]];
+        dw[k] = db[k] = 0.0f;
+      }
+      walk<T, V, 2, false>(wk, wk.in(a.x, a.x_sn), a.x_ss, wk.in(a.dout, a.dout_sn), a.dout_ss, [&](int s, const Vec<T, V>& q, const Vec<T, V>& e) {
+        float xh[V], du[V];
+        Draws<V> keep;
+        if constexpr (DROP) keep.draw(a.drop, (uint32_t)((int64_t)wk.i * a.S + s), wk.c);
+#pragma unroll
+        for (int k = 0; k < V; ++k) {
+          float v = q.get(k);
+          if constexpr (DROP) v = keep.kept(a.drop, k) ? v : 0.0f;
+          xh[k] = __builtin_fmaf(v, a.drop.scale, -mean[k]) * rstd[k];
+        }
+        grad_of<T, V>(a.act, ch.w, ch.b, e, xh, du);
+#pragma unroll
+        for (int k = 0; k < V; ++k) {
+          dw[k] = __builtin_fmaf(du[k], xh[k], dw[k]);
+          db[k] += du[k];
+        }
+      });
+      put(dw, db);
+      if constexpr (MANY) {
+#pragma unroll
+        for (int k = 0; k < V; ++k) {
+          all_w[k] += dw[k];
+          all_b[k] += db[k];
+        }
+      }
+    }
+    __syncthreads();
+    sum_rows([&](int q, float dw, float db) {   // row 0 of a channel is its team's own
+      if (!MANY && out) {
+        out[q] = dw;
+        out[a.C + q] = db;
+      }
       const float w = a.w ? a.w[wk.base + q] : 1.0f;
       dws[q] = dw * w;
       dbs[q] = db * w;
+    });
+    __syncthreads();
+    const int lanes = lanes_for(min(a.Cg, wk.local));
+    for (int t = threadIdx.x; wk.g0 + t / lanes <= wk.g1; t += 256) {
+      const int g = wk.g0 + t / lanes, l = t & (lanes - 1);
+      int lo, hi;
+      wk.channels_of(a, g, lo, hi);
+      float s1 = 0.0f, s2 = 0.0f;
+      for (int q = lo + l; q < hi; q += lanes) {
+        s1 += dbs[q];
+        s2 += dws[q];
+      }
+      s1 = team_sum(s1, lanes);
+      s2 = team_sum(s2, lanes);
+      if (l == 0) wk.share(a)[g - wk.g0] = make_float2(s1, s2);
     }
+    if constexpr (!MANY) return;
+    wk.i += gridDim.x / a.chunks;
+    if (wk.i >= a.n) break;
+    __syncthreads();
   }
+  if (!out) return;
   __syncthreads();
-  const int lanes = lanes_for(min(a.Cg, wk.local));
-  for (int t = threadIdx.x; wk.g0 + t / lanes <= wk.g1; t += 256) {
-    const int g = wk.g0 + t / lanes, l = t & (lanes - 1);
-    int lo, hi;
-    wk.channels_of(a, g, lo, hi);
-    float s1 = 0.0f, s2 = 0.0f;
-    for (int q = lo + l; q < hi; q += lanes) {
-      s1 += dbs[q];
-      s2 += dws[q];
-    }
-    s1 = team_sum(s1, lanes);
-    s2 = team_sum(s2, lanes);
-    if (l == 0) wk.share(a)[g - wk.g0] = make_float2(s1, s2);
-  }
+  if (wk.on) put(all_w, all_b);
+  __syncthreads();
+  sum_rows([&](int q, float dw, float db) {
+    out[q] = dw;
+    out[a.C + q] = db;
+  });
 }
 
 template <class T, int V, bool DROP>
@@ -758,6 +793,7 @@ static bool plan_block(const auv_norm* d, NormPlan& p) {
 #define AUV_NORM_TYPES(KERN, ...)                                                                               \
   (bf16 ? (p.V == 8 ? (const void*)KERN<__bf16, 8, __VA_ARGS__> : (const void*)KERN<__bf16, 1, __VA_ARGS__>) \
         : (p.V == 4 ? (const void*)KERN<float, 4, __VA_ARGS__> : (const void*)KERN<float, 1, __VA_ARGS__>))
+#define AUV_SUMS_KERNEL(MANY) (drop ? AUV_NORM_TYPES(k_norm_grad_sums, true, MANY) : AUV_NORM_TYPES(k_norm_grad_sums, false, MANY))
 #define AUV_CHUNK_KERNEL(KERN) (drop ? AUV_NORM_TYPES(KERN, true) : AUV_NORM_TYPES(KERN, false))
 #define AUV_BLOCK_GRAD(R, D) (merged ? AUV_NORM_TYPES(k_norm_block_grad, R, D, true) : AUV_NORM_TYPES(k_norm_block_grad, R, D, false))
 #define AUV_BLOCK_GRAD_DROP(R) (drop ? AUV_BLOCK_GRAD(R, true) : AUV_BLOCK_GRAD(R, false))
@@ -807,7 +843,10 @@ static int plan_chunks(const char* fn, const auv_norm* d, NormPlan& p) {
   p.chunks = (int)std::max<int64_t>(1, std::min<int64_t>(want, (d->s - 1) / (4 * step) + 1));
   p.per = (d->s - 1) / p.chunks + 1;
   p.chunks = (d->s - 1) / p.per + 1;
-  p.part_rows = (int64_t)d->n * p.chunks;
+  // Partial sums of the parameters' gradients: one row per chunk where that is little beside it (32 positions: an eighth of the
+  // tensor at most), else as many as workgroups are resident (three per CU), each over several samples.
+  const int64_t resident = std::max<int64_t>(1, (int64_t)3 * compute_units() / ((int64_t)p.tiles * p.chunks));
+  p.part_rows = p.chunks * (p.per >= 32 ? (int64_t)d->n : std::min<int64_t>(d->n, resident));
   return AUV_OK;
 }
 
@@ -923,7 +962,7 @@ int auv_norm_forward(const auv_norm* d, const auv_rows* y, void* work, void* str
   hipStream_t s = (hipStream_t)stream;
   if (p.form == NORM_ROWS) return launch_norm_rows(fn, a, p, bf16, false, 0, s);
   if (p.form == NORM_BLOCK) return launch_block(fn, d, p, a, false, s);
-  const dim3 grid((unsigned)p.part_rows, p.tiles);
+  const dim3 grid((unsigned)(d->n * p.chunks), p.tiles);
   const size_t lds = 2 * sizeof(float) * (256 / p.tile) * p.tile * p.V;
   if (int rc = launch_kernel(fn, AUV_CHUNK_KERNEL(k_norm_stats), grid, dim3(256), args, lds, s)) return rc;
   return launch_kernel(fn, AUV_CHUNK_KERNEL(k_norm_apply), grid, dim3(256), args, 2 * sizeof(float) * a.held, s);
@@ -953,7 +992,7 @@ int auv_norm_backward(const auv_norm* d, const auv_norm_grad* g, void* work, voi
   a.dx_ss = g->dx.ss;
   a.dw = g->dweight;
   a.db = g->dbias;
-  a.part = p.form != NORM_CHUNKS && !params ? nullptr : static_cast<float*>(work);
+  a.part = params ? static_cast<float*>(work) : nullptr;
   void* args[1] = {&a};
   hipStream_t s = (hipStream_t)stream;
   if (p.form == NORM_ROWS) {
@@ -963,10 +1002,11 @@ int auv_norm_backward(const auv_norm* d, const auv_norm_grad* g, void* work, voi
   } else if (p.form == NORM_BLOCK) {
     if (int rc = launch_block(fn, d, p, a, true, s)) return rc;
   } else {
-    const dim3 grid((unsigned)p.part_rows, p.tiles);
+    const dim3 sums((unsigned)p.part_rows, p.tiles), grid((unsigned)(d->n * p.chunks), p.tiles);
     const size_t lds = 2 * sizeof(float) * (256 / p.tile) * p.tile * p.V;
-    a.groups = a.part + part_floats(p, d->c, true);
-    if (int rc = launch_kernel(fn, AUV_CHUNK_KERNEL(k_norm_grad_sums), grid, dim3(256), args, lds, s)) return rc;
+    a.groups = static_cast<float*>(work) + part_floats(p, d->c, true);
+    const void* k = sums.x < grid.x ? AUV_SUMS_KERNEL(true) : AUV_SUMS_KERNEL(false);
+    if (int rc = launch_kernel(fn, k, sums, dim3(256), args, lds, s)) return rc;
     if (int rc = launch_kernel(fn, AUV_CHUNK_KERNEL(k_norm_grad_apply), grid, dim3(256), args, 2 * sizeof(float) * a.held, s))
       return rc;
   }

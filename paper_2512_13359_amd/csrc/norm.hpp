@@ -15,7 +15,7 @@ struct NormArgs {
   int64_t x_sn, x_ss, y_sn, y_ss, dout_sn, dout_ss, dx_sn, dx_ss;
   const float *w, *b;
   float *mean, *rstd;
-  float* part;    // backward: rows of partial sums of dw and db, [2][C] each
+  float* part;    // backward: rows of partial sums of dw and db, [2][C] each; null where neither is wanted
   float* groups;  // chunk form: [n][chunk][tile][held][2] moments (forward) or sums of d and d xhat (backward)
   float *dw, *db;
   float eps;

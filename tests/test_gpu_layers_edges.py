@@ -94,6 +94,18 @@ def test_scan_gradient_captured_and_on_two_streams():
         assert all(torch.equal(p, q) for p, q in zip(out, want[rep % 2 == 1])), rep
 
 
+@pytest.mark.parametrize("typ", ["fp32", "bf16"])
+@pytest.mark.parametrize("n, s, c, groups", [(700, 1, 4104, 1), (500, 1, 4101, 1), (600, 1, 4200, 2), (600, 5, 3000, 3), (800, 30, 272, 8), (40, 1, 40000, 4),
+                                             (1100, 1, 2052, 1)])
+def test_norm_of_many_samples_that_no_workgroup_holds(n, s, c, groups, typ):
+    """Workgroups that walk over several samples and keep the parameters' sums, and the same without parameters."""
+    require_gpu()
+    announce(f"norm many n={n} s={s} c={c} g={groups} {typ}")
+    check_norm(n, s, c, groups, typ, "silu", seed=c)
+    check_norm(n, s, c, groups, typ, "tanh", drop=6554, pitch=3, seed=n)
+    check_norm(n, s, c, groups, typ, "none", affine=False, seed=s)
+
+
 def test_norm_of_single_channels_in_wide_rows():
     """As many groups as channels over several tiles: each tile has shares of its own groups."""
     require_gpu()

@@ -9,12 +9,13 @@ P = 0x10000     # fake addresses: a refused call never follows them
 @pytest.mark.parametrize("n, s, c, groups", [(65536, 1, 8192, 1), (65536, 1, 4104, 1), (65536, 1, 4104, 27), (8192, 2, 65536, 8), (100000, 3, 6000, 5),
                                              (3000, 70, 8192, 64), (1, 1, 1 << 20, 1 << 20), (300, 1, 1 << 20, 1 << 10), (16, 8192, 4096, 4096), (5, 100, 3000, 1)])
 def test_norm_workspace_beside_its_tensors(n, s, c, groups, typ, size):
-    """A workspace is a small part of the tensor, beside what the results of a group take themselves: a tile has shares of its
-    own groups only."""
+    """A workspace is a small part of the tensor, beside what the results of a group and a parameter take themselves:
+    parameters' partial sums are bounded by the workgroups, not one row per sample, and a tile has shares of its own groups only."""
     from paper_2512_13359_amd import _abi as A
     d = A.AuvNorm(n=n, s=s, c=c, groups=groups, type=typ, act=0, eps=1e-5, x=P, x_sn=s * c, x_ss=c, mean=4 * P, rstd=5 * P)
-    x, stats = n * s * c * size, 8 * n * groups
-    # a chunk's shares beside the groups' statistics: a sample is at most 512 chunks and tiles, each
+    x, stats, params = n * s * c * size, 8 * n * groups, 8 * c
+    # one partial row at least; a chunk's shares beside the groups' statistics: a sample is at most 512 chunks and tiles, each
     # with at most one more group than its own
     shares = max(512, (n * s * c) // 2048) * 8 + stats * (min(512 // n, s) + 2)
     assert A.auv_norm_work_bytes(d, False) <= shares + x // 16
+    assert A.auv_norm_work_bytes(d, True) <= shares + x // 16 + params + (32 << 20)
