@@ -563,8 +563,9 @@ int auv_dropout(const auv_drop* drop, int32_t type, int32_t n, int32_t s, int32_
 enum { AUV_ACTIVATION_NONE = 0, AUV_ACTIVATION_RELU = 1, AUV_ACTIVATION_SILU = 2, AUV_ACTIVATION_TANH = 3 };
 
 typedef struct {
-  int32_t n, s, c, groups; /* groups divides c; n s c <= 2^40, c <= 2^20, n s and n groups <= 2^31 - 2^16, n < 2^24
-                              where s rows of c channels are more than 2048 pieces of 16 bytes */
+  int32_t n, s, c, groups; /* groups divides c; n s c <= 2^40, c <= 2^20, n s and n groups <= 2^31 - 2^16; n < 2^24
+                              where p ceil(s / 4) > 512 with p the 16-byte pieces of a row (the channels of one that
+                              holds none); rows in groups of 1024 channels at most may be more */
   int32_t type, act;
   float eps;               /* >= 0 */
   auv_rows x;

@@ -19,3 +19,15 @@ def test_norm_workspace_beside_its_tensors(n, s, c, groups, typ, size):
     shares = max(512, (n * s * c) // 2048) * 8 + stats * (min(512 // n, s) + 2)
     assert A.auv_norm_work_bytes(d, False) <= shares + x // 16
     assert A.auv_norm_work_bytes(d, True) <= shares + x // 16 + params + (32 << 20)
+
+
+@pytest.mark.parametrize("s, c, groups, taken", [(1, 4096, 1, True), (1, 4104, 1, False), (4, 4096, 2, True), (5, 2048, 1, True), (5, 2056, 1, False),
+                                                 (9, 1368, 1, False), (64, 256, 2, True), (65, 256, 2, False), (1, 8192, 8, True)])
+def test_norm_of_more_samples_than_a_launch_takes(s, c, groups, taken):
+    """The header's bound: 2^24 samples where p ceil(s / 4) > 512 with p the 16-byte pieces of a row."""
+    from paper_2512_13359_amd import _abi as A
+    assert taken == (-(-c // 8) * -(-s // 4) <= 512) or groups == 8
+    d = A.AuvNorm(n=1 << 24, s=s, c=c, groups=groups, type=A.AUV_BF16, act=0, eps=1e-5, x=P, x_sn=s * c, x_ss=c, mean=4 * P, rstd=5 * P)
+    assert (A.lib.auv_norm_work_bytes(d, 1) >= 0) == taken, A.auv_last_error()
+    if not taken:
+        assert "2^24" in A.auv_last_error()
