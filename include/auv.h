@@ -481,7 +481,7 @@ int auv_shac_window(auv_env* env, const auv_shac_config* cfg, const auv_mlp* pol
  * buffer are separate tensors.  Pointers are aligned to their elements, `work` to 16 bytes.
  * AUV_EINVAL, nothing enqueued: sizes below 1 or beyond the limits given, an unknown type, kind
  * or activation, NULL or misaligned pointers, negative strides, an output whose elements share
- * memory, an output at an input's address. */
+ * memory, an output at the address of an input or another output. */
 enum { AUV_FP32 = 0, AUV_BF16 = 1 };
 
 /* Gated linear recurrence.  Of n sequences with c channels each, from the state s_{-1} = h0:

@@ -5,9 +5,27 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include <initializer_list>
+
 #include "auv_internal.hpp"
 
 namespace auv {
+
+// A call's tensors by name; none of the outputs may start where an input or another output does.
+struct Named {
+  const char* name;
+  const void* p;   // may be null
+};
+inline int check_apart(const char* fn, std::initializer_list<Named> outputs, std::initializer_list<Named> inputs) {
+  for (const Named* o = outputs.begin(); o != outputs.end(); ++o) {
+    if (!o->p) continue;
+    for (const Named& i : inputs)
+      if (i.p == o->p) return set_error(AUV_EINVAL, "%s: '%s' is the memory of '%s', an input", fn, o->name, i.name);
+    for (const Named* q = outputs.begin(); q != o; ++q)
+      if (q->p == o->p) return set_error(AUV_EINVAL, "%s: '%s' and '%s' are the same memory", fn, q->name, o->name);
+  }
+  return AUV_OK;
+}
 
 // A kernel by its address; `fn` is the entry point named in the error.
 inline int launch_kernel(const char* fn, const void* kernel, dim3 grid, dim3 block, void** args, size_t lds, hipStream_t s) {

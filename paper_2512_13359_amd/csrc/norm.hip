@@ -947,7 +947,8 @@ int auv_norm_forward(const auv_norm* d, const auv_rows* y, void* work, void* str
   if (!y || !d->mean || !d->rstd) return set_error(AUV_EINVAL, "%s: NULL argument", fn);
   if (int rc = check_rows(fn, "x", d->x, d->type, d->n, d->s, d->c, false)) return rc;
   if (int rc = check_rows(fn, "y", *y, d->type, d->n, d->s, d->c, true)) return rc;
-  if (y->p == d->x.p) return set_error(AUV_EINVAL, "%s: 'y' is the memory of 'x'", fn);
+  if (int rc = check_apart(fn, {{"y", y->p}, {"mean", d->mean}, {"rstd", d->rstd}}, {{"x", d->x.p}, {"weight", d->weight}, {"bias", d->bias}}))
+    return rc;
   const bool bf16 = d->type == AUV_BF16, drop = d->drop && d->drop->drop;
   NormPlan p{};
   if (int rc = plan(fn, d, d->x.ss == d->c && y->ss == d->c, false, p)) return rc;
@@ -975,10 +976,11 @@ int auv_norm_backward(const auv_norm* d, const auv_norm_grad* g, void* work, voi
   if (int rc = check_rows(fn, "x", d->x, d->type, d->n, d->s, d->c, false)) return rc;
   if (int rc = check_rows(fn, "dout", g->dout, d->type, d->n, d->s, d->c, false)) return rc;
   if (int rc = check_rows(fn, "dx", g->dx, d->type, d->n, d->s, d->c, true)) return rc;
-  if (g->dx.p == d->x.p || g->dx.p == g->dout.p) return set_error(AUV_EINVAL, "%s: 'dx' is an input's memory", fn);
   if ((reinterpret_cast<uintptr_t>(g->dweight) | reinterpret_cast<uintptr_t>(g->dbias)) & 3u)
     return set_error(AUV_EINVAL, "%s: 'dweight' or 'dbias' is not 4-byte aligned", fn);
-  if (g->dweight && g->dweight == g->dbias) return set_error(AUV_EINVAL, "%s: 'dweight' and 'dbias' are the same memory", fn);
+  if (int rc = check_apart(fn, {{"dx", g->dx.p}, {"dweight", g->dweight}, {"dbias", g->dbias}},
+                           {{"x", d->x.p}, {"dout", g->dout.p}, {"weight", d->weight}, {"bias", d->bias}, {"mean", d->mean}, {"rstd", d->rstd}}))
+    return rc;
   if (!work || !aligned16(work)) return set_error(AUV_EINVAL, "%s: 'work' is NULL or not 16-byte aligned", fn);
   const bool bf16 = d->type == AUV_BF16, drop = d->drop && d->drop->drop, params = g->dweight || g->dbias;
   NormPlan p{};

@@ -340,9 +340,12 @@ int auv_scan_forward(const auv_scan* d, void* work, void* stream) {
   if (int rc = check_seq(fn, "gate", d->gate, d, false)) return rc;
   if (int rc = check_seq(fn, "x", d->x, d, false)) return rc;
   if (int rc = check_seq(fn, "h", d->h, d, true)) return rc;
-  if (d->h.p == d->gate.p || d->h.p == d->x.p) return set_error(AUV_EINVAL, "%s: 'h' is an input's memory", fn);
   if (int rc = check_state(fn, "h0", d->h0, d, false)) return rc;
   if (int rc = check_state(fn, "last", d->last, d, true)) return rc;
+  if (int rc = check_apart(fn, {{"h", d->h.p}, {"last", d->last.p}},
+                           {{"gate", d->gate.p}, {"x", d->x.p}, {"done", d->done}, {"lens", d->lens}}))
+    return rc;
+  if (int rc = check_apart(fn, {{"h", d->h.p}}, {{"h0", d->h0.p}})) return rc;   // 'last' may be 'h0'
   if (d->last.p && d->last.p == d->h0.p && (d->last.sn != d->h0.sn || d->last.sc != d->h0.sc))
     return set_error(AUV_EINVAL, "%s: 'last' is the memory of 'h0' with other strides", fn);
   ScanArgs a{};
@@ -366,15 +369,13 @@ int auv_scan_backward(const auv_scan* d, const auv_scan_grad* g, void* work, voi
     if (int rc = check_seq(fn, "dout", g->dout, d, false)) return rc;
   if (int rc = check_seq(fn, "dgate", g->dgate, d, true)) return rc;
   if (int rc = check_seq(fn, "dx", g->dx, d, true)) return rc;
-  const void* in[4] = {d->gate.p, d->x.p, d->h.p, g->dout.p};
-  for (const void* p : in)
-    if (g->dgate.p == p || g->dx.p == p) return set_error(AUV_EINVAL, "%s: 'dgate' or 'dx' is an input's memory", fn);
-  if (g->dgate.p == g->dx.p) return set_error(AUV_EINVAL, "%s: 'dgate' and 'dx' are the same memory", fn);
   if (int rc = check_state(fn, "h0", d->h0, d, false)) return rc;
   if (int rc = check_state(fn, "dlast", g->dlast, d, false)) return rc;
   if (int rc = check_state(fn, "dh0", g->dh0, d, true)) return rc;
-  if (g->dh0.p && (g->dh0.p == d->h0.p || g->dh0.p == g->dlast.p))
-    return set_error(AUV_EINVAL, "%s: 'dh0' is an input's memory", fn);
+  if (int rc = check_apart(fn, {{"dgate", g->dgate.p}, {"dx", g->dx.p}, {"dh0", g->dh0.p}},
+                           {{"gate", d->gate.p}, {"x", d->x.p}, {"h", d->h.p}, {"dout", g->dout.p}, {"done", d->done}, {"lens", d->lens},
+                            {"h0", d->h0.p}, {"dlast", g->dlast.p}}))
+    return rc;
   ScanArgs a{};
   ScanShape sh{};
   backward_args(d, g, a, sh);

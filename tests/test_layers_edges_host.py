@@ -31,3 +31,56 @@ def test_norm_of_more_samples_than_a_launch_takes(s, c, groups, taken):
     assert (A.lib.auv_norm_work_bytes(d, 1) >= 0) == taken, A.auv_last_error()
     if not taken:
         assert "2^24" in A.auv_last_error()
+
+
+def _scan(A, **kw):
+    d = dict(T=4, n=3, c=8, type=A.AUV_FP32, kind=0, gate=P, gate_st=24, gate_sn=8, gate_sc=1, x=2 * P, x_st=24, x_sn=8, x_sc=1,
+             h=3 * P, h_st=24, h_sn=8, h_sc=1, done=4 * P, lens=5 * P, h0=6 * P, h0_sn=8, h0_sc=1, last=7 * P, last_sn=8, last_sc=1)
+    d.update(kw)
+    return A.AuvScan(**d)
+
+
+def pairs(outs, others):
+    """Every output of a call with every other tensor of it; the exception is a state updated in place."""
+    return [(o, i) for o in outs for i in others if o != i and (o, i) != ("last", "h0")]
+
+
+@pytest.mark.parametrize("out, other", pairs(("h", "last"), ("gate", "x", "done", "lens", "h0", "h", "last")))
+def test_scan_forward_refuses_an_output_over_another_tensor(out, other):
+    from paper_2512_13359_amd import _abi as A
+    d = _scan(A)
+    rc = A.lib.auv_scan_forward(_scan(A, **{out: getattr(d, other)}), None, None)
+    assert rc == A.AUV_EINVAL and f"'{out}'" in A.auv_last_error() and f"'{other}'" in A.auv_last_error(), A.auv_last_error()
+
+
+@pytest.mark.parametrize("out, other", pairs(("dgate", "dx", "dh0"), ("gate", "x", "h", "dout", "done", "lens", "h0", "dlast", "dgate", "dx", "dh0")))
+def test_scan_backward_refuses_an_output_over_another_tensor(out, other):
+    from paper_2512_13359_amd import _abi as A
+    g = dict(dout=8 * P, dout_st=24, dout_sn=8, dout_sc=1, dlast=9 * P, dlast_sn=8, dlast_sc=1, dgate=10 * P, dgate_st=24, dgate_sn=8,
+             dgate_sc=1, dx=11 * P, dx_st=24, dx_sn=8, dx_sc=1, dh0=12 * P, dh0_sn=8, dh0_sc=1)
+    d = _scan(A, last=None)
+    g[out] = g[other] if other in g else getattr(d, other)
+    rc = A.lib.auv_scan_backward(d, A.AuvScanGrad(**g), None, None)
+    assert rc == A.AUV_EINVAL and f"'{out}'" in A.auv_last_error() and f"'{other}'" in A.auv_last_error(), A.auv_last_error()
+
+
+@pytest.mark.parametrize("out, other", pairs(("y", "mean", "rstd"), ("x", "weight", "bias", "y", "mean", "rstd")))
+def test_norm_forward_refuses_an_output_over_another_tensor(out, other):
+    from paper_2512_13359_amd import _abi as A
+    t = {k: (i + 1) * P for i, k in enumerate(("x", "weight", "bias", "y", "mean", "rstd"))}
+    t[out] = t[other]
+    d = A.AuvNorm(n=2, s=3, c=8, groups=2, type=0, act=0, eps=1e-5, x=t["x"], x_sn=24, x_ss=8, weight=t["weight"], bias=t["bias"],
+                  mean=t["mean"], rstd=t["rstd"])
+    rc = A.lib.auv_norm_forward(d, A.AuvRows(t["y"], 24, 8), None, None)
+    assert rc == A.AUV_EINVAL and f"'{out}'" in A.auv_last_error() and f"'{other}'" in A.auv_last_error(), A.auv_last_error()
+
+
+@pytest.mark.parametrize("out, other", pairs(("dx", "dweight", "dbias"), ("x", "dout", "weight", "bias", "mean", "rstd", "dx", "dweight", "dbias")))
+def test_norm_backward_refuses_an_output_over_another_tensor(out, other):
+    from paper_2512_13359_amd import _abi as A
+    t = {k: (i + 1) * P for i, k in enumerate(("x", "weight", "bias", "mean", "rstd", "dout", "dx", "dweight", "dbias"))}
+    t[out] = t[other]
+    d = A.AuvNorm(n=2, s=3, c=8, groups=2, type=0, act=0, eps=1e-5, x=t["x"], x_sn=24, x_ss=8, weight=t["weight"], bias=t["bias"],
+                  mean=t["mean"], rstd=t["rstd"])
+    rc = A.lib.auv_norm_backward(d, A.AuvNormGrad(t["dout"], 24, 8, t["dx"], 24, 8, t["dweight"], t["dbias"]), 20 * P, None)
+    assert rc == A.AUV_EINVAL and f"'{out}'" in A.auv_last_error() and f"'{other}'" in A.auv_last_error(), A.auv_last_error()
