@@ -5,7 +5,8 @@ gradient (auv_scan_*, auv_norm_*, auv_dropout).  Argument checks, allocation and
 Outputs and workspaces are torch allocations made on the stream that the call runs on: the current
 stream of the tensors' device, or `stream`.  Nothing is kept between calls, so calls may be captured
 into a graph.  The functions are not part of torch's autograd: gradients come from the *_backward
-functions.  Wrong arguments raise AuvError before anything is enqueued."""
+functions, and a tensor that requires grad is refused where torch records (call under torch.no_grad(), or
+from a torch.autograd.Function, whose forward and backward do not record).  Wrong arguments raise AuvError before anything is enqueued."""
 from __future__ import annotations
 
 import struct
@@ -44,6 +45,15 @@ def _like(fn, name, t, shape, dtype, index, contiguous=False):
     if t.get_device() != index:
         _refuse(fn, f"{name} is on another device than x: {t.device}")
     _refuse(fn, f"{name} must be contiguous")
+
+
+def _unrecorded(fn, *tensors):
+    """Results are cut from torch's graph: refused where a gradient would be lost by it."""
+    if torch.is_grad_enabled():
+        for t in tensors:
+            if t is not None and t.requires_grad:
+                _refuse(fn, "a tensor requires grad and the result would not: call under torch.no_grad(), gradients come from "
+                            "the *_backward functions")
 
 
 def _here(fn, x, stream) -> bool:
@@ -118,6 +128,7 @@ def scan_forward(gate, x, *, kind="sigmoid", done=None, lens=None, h0=None, out=
     h has x's type and memory order, or is `out`; last = s_{T-1} and h0 are float32 [n][c].  One step
     (T = 1) is the form for a controller: pass `last` back as the next h0."""
     fn = "scan_forward"
+    _unrecorded(fn, gate, x, h0, out)
     head = _scan(fn, gate, x, kind, done, lens, h0)
     if out is not None:
         _like(fn, "out", out, x.shape, x.dtype, x.get_device())
@@ -134,10 +145,12 @@ def scan_forward(gate, x, *, kind="sigmoid", done=None, lens=None, h0=None, out=
 def scan_backward(gate, x, h, *, dout=None, dh_last=None, kind="sigmoid", done=None, lens=None, h0=None, out=None,
                   stream=None):
     """Gradients (dgate, dx, dh0) of scan_forward from those of its results, dout (of h) and dh_last
-    (of last); None stands for zero.  h is scan_forward's result, the other arguments its own.
+    (of last); None stands for zero.  h is scan_forward's result, the other arguments its own.  States are
+    float32 here too: those of bfloat16 tensors are formed again from the inputs, not read from the rounded h.
     dgate and dx have x's type (zero at held steps), or are the pair `out`: the halves of one
     buffer, say, where gate and x are the halves of one projection.  dh0 is float32 [n][c]."""
     fn = "scan_backward"
+    _unrecorded(fn, gate, x, h, dout, dh_last, h0, *(out or ()))
     head = _scan(fn, gate, x, kind, done, lens, h0)
     _like(fn, "h", h, x.shape, x.dtype, x.get_device())
     if dout is not None:
@@ -190,6 +203,7 @@ def dropout(x, drop, add=None, *, out=None, stream=None):
     No mask is stored: the gradient is dropout of the gradient with the same `drop`.  `out` may be x or
     add itself."""
     fn = "dropout"
+    _unrecorded(fn, x, add, out)
     n, s, c = _sizes(fn, x)
     if add is not None:
         _like(fn, "add", add, x.shape, x.dtype, x.get_device())
@@ -225,6 +239,7 @@ def norm_forward(x, groups, *, weight=None, bias=None, eps=1e-5, act="none", dro
     "silu", "tanh".  With `drop` (make_drop) x is dropped out first, its mask never stored.  mean and
     rstd are float32 [n][groups]; y has x's type, or is `out`."""
     fn = "norm_forward"
+    _unrecorded(fn, x, weight, bias, out)
     d = _norm(fn, x, groups, weight, bias, eps, act, drop)
     if out is not None:
         _like(fn, "out", out, x.shape, x.dtype, x.get_device())
@@ -245,6 +260,7 @@ def norm_backward(x, groups, mean, rstd, dout, *, weight=None, bias=None, act="n
     other arguments its own.  dx has x's type, or is `out`; dweight is None where weight is, dbias
     where bias is, else float32 [c]."""
     fn = "norm_backward"
+    _unrecorded(fn, x, mean, rstd, dout, weight, bias, out)
     d = _norm(fn, x, groups, weight, bias, 0.0, act, drop)
     for name, t in (("mean", mean), ("rstd", rstd)):
         _like(fn, name, t, (d.n, groups), torch.float32, x.get_device(), True)

@@ -84,3 +84,24 @@ def test_norm_backward_refuses_an_output_over_another_tensor(out, other):
                   mean=t["mean"], rstd=t["rstd"])
     rc = A.lib.auv_norm_backward(d, A.AuvNormGrad(t["dout"], 24, 8, t["dx"], 24, 8, t["dweight"], t["dbias"]), 20 * P, None)
     assert rc == A.AUV_EINVAL and f"'{out}'" in A.auv_last_error() and f"'{other}'" in A.auv_last_error(), A.auv_last_error()
+
+
+def test_functions_refuse_tensors_whose_gradient_would_be_lost():
+    """Results are no part of torch's graph: a tensor that requires grad is refused, unless torch does not record."""
+    import paper_2512_13359_amd as M
+    x, w, st = torch.zeros(4, 3, 8), torch.zeros(8), torch.zeros(3, 8)
+    leaf = lambda t: t.clone().requires_grad_()  # noqa: E731
+    d, stat = M.make_drop(0.1, 1), torch.zeros(4, 2)
+    calls = [lambda: M.scan_forward(leaf(x), x), lambda: M.scan_forward(x, leaf(x)), lambda: M.scan_forward(x, x, h0=leaf(st)),
+             lambda: M.scan_forward(x, x, out=leaf(x)), lambda: M.scan_backward(x, leaf(x), x), lambda: M.scan_backward(x, x, leaf(x)),
+             lambda: M.scan_backward(x, x, x, dout=leaf(x)), lambda: M.scan_backward(x, x, x, dh_last=leaf(st)),
+             lambda: M.scan_backward(x, x, x, out=(x, leaf(x))), lambda: M.dropout(leaf(x), d), lambda: M.dropout(x, d, leaf(x)),
+             lambda: M.dropout(x, d, out=leaf(x)), lambda: M.norm_forward(leaf(x), 2), lambda: M.norm_forward(x, 2, weight=leaf(w)),
+             lambda: M.norm_forward(x, 2, bias=torch.nn.Parameter(w)), lambda: M.norm_forward(x, 2, out=leaf(x)),
+             lambda: M.norm_backward(leaf(x), 2, stat, stat, x), lambda: M.norm_backward(x, 2, stat, stat, leaf(x)),
+             lambda: M.norm_backward(x, 2, stat, stat, x, weight=leaf(w))]
+    for k, f in enumerate(calls):
+        with pytest.raises(M.AuvError, match="requires grad"):
+            f()
+        with torch.no_grad(), pytest.raises(M.AuvError, match="on a GPU"):      # taken as far as the next check
+            f()
