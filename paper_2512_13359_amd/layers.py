@@ -61,7 +61,11 @@ def _here(fn, x, stream) -> bool:
     index = x.get_device()
     if index < 0:
         _refuse(fn, f"tensors must be on a GPU, x is on {x.device}")
-    return stream is None and index == torch.cuda.current_device()
+    if stream is not None:
+        if stream.device.index != index:    # entering it would make its device the current one
+            _refuse(fn, f"the stream is {stream.device}'s, x is on {x.device}")
+        return False
+    return index == torch.cuda.current_device()
 
 
 def _packed(fn, kind, layout, *words):

@@ -143,3 +143,21 @@ def test_norm_inside_an_autograd_function():
     for p, q in zip(got, L.norm_grad(X, 2, mean, rstd, f64(dy).reshape(50, 1, 48), Wt, B, "silu")):
         # sums of 24 and 50 terms and some thirty roundings of each, relative to the largest value
         assert np.abs(f64(p).reshape(q.shape) - q).max() <= 256 * U * np.abs(q).max()
+
+
+def test_stream_of_another_device_is_refused():
+    """It would be entered and left again for the current stream of x's device, on which the call then ran."""
+    require_gpu()
+    from types import SimpleNamespace
+
+    from paper_2512_13359_amd import AuvError, dropout, make_drop, norm_backward, norm_forward, scan_backward, scan_forward
+    other = SimpleNamespace(device=torch.device("cuda", 1))     # all that is looked at
+    x = torch.zeros(4, 3, 8, device="cuda")
+    stat = torch.zeros(4, 2, device="cuda")
+    for f in (lambda **k: scan_forward(x, x, **k), lambda **k: scan_backward(x, x, x, **k), lambda **k: dropout(x, make_drop(0.5, 1), **k),
+              lambda **k: norm_forward(x, 2, **k), lambda **k: norm_backward(x, 2, stat, stat, x, **k)):
+        with pytest.raises(AuvError, match="stream"):
+            f(stream=other)
+        f(stream=torch.cuda.Stream())
+        f(stream=torch.cuda.current_stream())
+    torch.cuda.synchronize()
