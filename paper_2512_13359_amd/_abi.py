@@ -107,7 +107,8 @@ class AuvScanGrad(ctypes.Structure):
 
 
 class AuvDrop(ctypes.Structure):
-    _fields_ = [("seed", ctypes.c_uint64)] + [(k, ctypes.c_uint32) for k in ("step", "site", "row0", "drop")]
+    _fields_ = [("seed", ctypes.c_uint64)] + [(k, ctypes.c_uint32) for k in ("step", "site", "row0", "drop")] + [("counter", _vp)]
+    tensor = None   # the counter's, held while the structure is
 
 
 class AuvRows(ctypes.Structure):
@@ -438,15 +439,23 @@ def make_shac_buffers(**kw) -> AuvShacBuffers:
     return AuvShacBuffers(**{k: ptr(v) for k, v in kw.items()})
 
 
-def make_drop(p: float, seed: int, step: int = 0, site: int = 0, row0: int = 0) -> AuvDrop:
+def make_drop(p: float, seed: int, step: int = 0, site: int = 0, row0: int = 0, counter=None) -> AuvDrop:
     """Dropout with probability p (rounded to 65536ths): the draws of update `step` and layer `site`
-    (below 2^24) under a 64-bit seed; row0: global number of the tensors' first row."""
+    (below 2^24) under a 64-bit seed; row0: global number of the tensors' first row.  counter: an int32
+    tensor of one element on the GPU, added to step when a call runs.  A call captured into a graph draws the
+    same elements at every replay unless a counter that the program advances tells them apart."""
     if not 0.0 <= p < 1.0 or round(p * 65536) >= 65536:
         raise AuvError(AUV_EINVAL, f"make_drop: p must be in [0, 1) and below 1 in 65536ths, got {p}")
     for name, v, bits in (("seed", seed, 64), ("step", step, 32), ("site", site, 24), ("row0", row0, 32)):
         if not 0 <= v < 1 << bits:
             raise AuvError(AUV_EINVAL, f"make_drop: {name} must be in [0, 2^{bits}), got {v}")
-    return AuvDrop(seed, step, site, row0, round(p * 65536))
+    d = AuvDrop(seed, step, site, row0, round(p * 65536))
+    if counter is not None:
+        if str(counter.dtype) != "torch.int32" or counter.numel() != 1 or counter.get_device() < 0:
+            raise AuvError(AUV_EINVAL, f"make_drop: counter must be an int32 tensor of one element on a GPU, got {counter.dtype} of "
+                                       f"{tuple(counter.shape)} on {counter.device}")
+        d.counter, d.tensor = counter.data_ptr(), counter
+    return d
 
 
 def make_rollout_buffers(**kw) -> AuvRolloutBuffers:

@@ -67,6 +67,7 @@ __global__ __launch_bounds__(256) void k_dropout(DropoutArgs a) {
     }
   }
   if (a.drop.drop) {
+    a.drop.count();
     Draws<8> keep;
     keep.draw(a.drop, row, c);
 #pragma unroll
@@ -100,6 +101,7 @@ DropArgs drop_args(const auv_drop* d) {
     D.tag = 3u | d->site << 8;
     D.row0 = d->row0;
     D.drop = d->drop;
+    D.counter = d->counter;
     D.scale = 65536.0f / (float)(65536u - d->drop);
   }
   return D;
@@ -108,6 +110,7 @@ DropArgs drop_args(const auv_drop* d) {
 int check_drop(const char* fn, const auv_drop* d, int64_t rows) {
   if (d->site >= (1u << 24)) return set_error(AUV_EINVAL, "%s: dropout site must be below 2^24", fn);
   if (d->drop >= 65536u) return set_error(AUV_EINVAL, "%s: dropout probability must be below 65536 / 65536", fn);
+  if (reinterpret_cast<uintptr_t>(d->counter) & 3u) return set_error(AUV_EINVAL, "%s: dropout's counter is not 4-byte aligned", fn);
   if (rows + d->row0 > ((int64_t)1 << 32)) return set_error(AUV_EINVAL, "%s: row0 + n s exceeds 2^32", fn);
   return AUV_OK;
 }

@@ -10,6 +10,12 @@ struct DropArgs {
   uint32_t key0, key1, step, tag, row0;
   uint32_t drop;   // dropped below this; 0: keep all (and draw nothing)
   float scale;     // 65536 / (65536 - drop)
+  const uint32_t* counter;
+
+  // first thing in a kernel that draws
+  __device__ __forceinline__ void count() {
+    if (counter) step += *counter;
+  }
 };
 
 // host side (dropout.hip): arguments of a launch; d may be null

@@ -111,6 +111,7 @@ __device__ __forceinline__ void group_sums(const NormArgs& a, const float* cols,
 
 template <class T, int V, int R, bool DROP>
 __global__ __launch_bounds__(512) void k_norm_block(NormArgs a) {
+  if constexpr (DROP) a.drop.count();
   extern __shared__ float lds[];
   const BlockTeam<T, V, R> tm(a);
   const int width = a.pack * a.C, all = a.pack * a.G;
@@ -202,6 +203,7 @@ __global__ __launch_bounds__(512) void k_norm_block(NormArgs a) {
 // Merged: the V channels of a thread are of one group, whose values are held once.
 template <class T, int V, int R, bool DROP, bool MERGED>
 __global__ __launch_bounds__(512) void k_norm_block_grad(NormArgs a) {
+  if constexpr (DROP) a.drop.count();
   extern __shared__ float lds[];
   constexpr int VG = MERGED ? 1 : V;   // groups of a thread
   const BlockTeam<T, V, R> tm(a);
@@ -424,6 +426,7 @@ __device__ __forceinline__ void walk(const Walker<T, V>& wk, const T* x, int64_t
 
 template <class T, int V, bool DROP>
 __global__ __launch_bounds__(256) void k_norm_stats(NormArgs a) {
+  if constexpr (DROP) a.drop.count();
   extern __shared__ float red[];   // means and squares about them, [2][step][tile V]
   const Walker<T, V> wk(a);
   const int width = a.tile * V;
@@ -504,6 +507,7 @@ template <int V> struct ChannelValues {
 
 template <class T, int V, bool DROP>
 __global__ __launch_bounds__(256) void k_norm_apply(NormArgs a) {
+  if constexpr (DROP) a.drop.count();
   extern __shared__ float lds[];   // mean and rstd of the tile's groups
   const Walker<T, V> wk(a);
   const int groups = wk.g1 - wk.g0 + 1;
@@ -555,6 +559,7 @@ __global__ __launch_bounds__(256) void k_norm_apply(NormArgs a) {
 // 65536 rows of 8192 bf16 channels leave 256 partial rows (17 MB), not one each.
 template <class T, int V, bool DROP, bool MANY>
 __global__ __launch_bounds__(256) void k_norm_grad_sums(NormArgs a) {
+  if constexpr (DROP) a.drop.count();
   extern __shared__ float red[];   // [2][step][tile V], then sums in their first rows
   Walker<T, V> wk(a);
   const int width = a.tile * V;
@@ -665,6 +670,7 @@ __global__ __launch_bounds__(256) void k_norm_grad_sums(NormArgs a) {
 
 template <class T, int V, bool DROP>
 __global__ __launch_bounds__(256) void k_norm_grad_apply(NormArgs a) {
+  if constexpr (DROP) a.drop.count();
   extern __shared__ float lds[];   // means of d and of d xhat of the tile's groups
   const Walker<T, V> wk(a);
   const int groups = wk.g1 - wk.g0 + 1;

@@ -49,6 +49,7 @@ template <class T, int V, int NV> struct RowTeam {
 // products per eight elements fill the VALU beside it.
 template <class T, int V, int NV, bool DROP, bool FULL>
 __global__ __launch_bounds__(256) void k_norm_rows(NormArgs a) {
+  if constexpr (DROP) a.drop.count();
   constexpr bool full = FULL;   // every lane's vectors are whole and its own
   const RowTeam<T, V, NV> tm(a);
   const int per = 256 / a.lanes;
@@ -128,6 +129,7 @@ __global__ __launch_bounds__(256) void k_norm_rows(NormArgs a) {
 // Bound by HBM, x and dy in and dx out: the same in 83 us with the parameters' sum (4.8 TB/s), with dropout 89.
 template <class T, int V, int NV, bool DROP, bool FULL>
 __global__ __launch_bounds__(256) void k_norm_rows_grad(NormArgs a) {
+  if constexpr (DROP) a.drop.count();
   constexpr bool full = FULL;   // every lane's vectors are whole and its own
   const RowTeam<T, V, NV> tm(a);
   const int per = 256 / a.lanes;

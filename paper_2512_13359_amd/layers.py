@@ -4,9 +4,11 @@ gradient (auv_scan_*, auv_norm_*, auv_dropout).  Argument checks, allocation and
 
 Outputs and workspaces are torch allocations made on the stream that the call runs on: the current
 stream of the tensors' device, or `stream`.  Nothing is kept between calls, so calls may be captured
-into a graph.  The functions are not part of torch's autograd: gradients come from the *_backward
-functions, and a tensor that requires grad is refused where torch records (call under torch.no_grad(), or
-from a torch.autograd.Function, whose forward and backward do not record).  Wrong arguments raise AuvError before anything is enqueued."""
+into a graph; a captured dropout draws the same elements at every replay unless make_drop's counter
+tells the replays apart.  The functions are not part of torch's autograd: gradients come from the
+*_backward functions, and a tensor that requires grad is refused where torch records (call under
+torch.no_grad(), or from a torch.autograd.Function, whose forward and backward do not record).  Wrong
+arguments raise AuvError before anything is enqueued."""
 from __future__ import annotations
 
 import struct
@@ -54,6 +56,13 @@ def _unrecorded(fn, *tensors):
             if t is not None and t.requires_grad:
                 _refuse(fn, "a tensor requires grad and the result would not: call under torch.no_grad(), gradients come from "
                             "the *_backward functions")
+
+
+def _drop_here(fn, drop, x):
+    if not isinstance(drop, A.AuvDrop):
+        _refuse(fn, f"drop must be one of make_drop, got {type(drop).__name__}")
+    if drop.tensor is not None and drop.tensor.get_device() != x.get_device():
+        _refuse(fn, f"drop's counter is on another device than x: {drop.tensor.device}")
 
 
 def _here(fn, x, stream) -> bool:
@@ -209,6 +218,7 @@ def dropout(x, drop, add=None, *, out=None, stream=None):
     fn = "dropout"
     _unrecorded(fn, x, add, out)
     n, s, c = _sizes(fn, x)
+    _drop_here(fn, drop, x)
     if add is not None:
         _like(fn, "add", add, x.shape, x.dtype, x.get_device())
     if out is not None:
@@ -225,6 +235,8 @@ def dropout(x, drop, add=None, *, out=None, stream=None):
 def _norm(fn, x, groups, weight, bias, eps, act, drop):
     """The structure without mean and rstd; the callers hold `drop` while it is in use."""
     n, s, c = _sizes(fn, x)
+    if drop is not None:
+        _drop_here(fn, drop, x)
     if weight is not None:
         _like(fn, "weight", weight, (c,), torch.float32, x.get_device(), True)
     if bias is not None:

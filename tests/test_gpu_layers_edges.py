@@ -161,3 +161,43 @@ def test_stream_of_another_device_is_refused():
         f(stream=torch.cuda.Stream())
         f(stream=torch.cuda.current_stream())
     torch.cuda.synchronize()
+
+
+@pytest.mark.parametrize("n, s, c, groups", [(300, 1, 200, 1), (40, 1, 90, 6), (9, 20, 24, 3), (3, 2500, 20, 2), (300, 1, 4200, 2)])
+def test_captured_dropout_draws_by_its_counter(n, s, c, groups):
+    """A counter on the device tells the replays of a captured training step apart, in every form of the norm: replay k is the eager
+    step k.  Without one every replay draws what the captured call drew."""
+    require_gpu()
+    from paper_2512_13359_amd import dropout, make_drop, norm_backward, norm_forward
+    announce(f"dropout counter n={n} s={s} c={c} g={groups}")
+    g = torch.Generator(device="cuda")
+    g.manual_seed(c)
+    x, dy = (torch.randn(n, s, c, generator=g, device="cuda") for _ in range(2))
+    w, b = torch.randn(c, generator=g, device="cuda"), torch.randn(c, generator=g, device="cuda")
+
+    def step(**at):
+        d = make_drop(0.3, 99, site=2, **at)
+        v = dropout(x, d, x)
+        y, mean, rstd = norm_forward(v, groups, weight=w, bias=b, act="tanh", drop=d)
+        return (v, y, mean, rstd, *norm_backward(v, groups, mean, rstd, dy, weight=w, bias=b, act="tanh", drop=d))
+
+    first = 0xFFFFFFFE      # the sum passes 2^32
+    eager = [step(step=(first + k) % 2 ** 32) for k in range(5)]
+    assert not torch.equal(eager[0][0], eager[1][0]) and not torch.equal(eager[0][1], eager[2][1])
+    counter = torch.zeros(1, dtype=torch.int32, device="cuda")
+    torch.cuda.synchronize()
+    graph, fixed = torch.cuda.CUDAGraph(), torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = step(step=first, counter=counter)
+        counter.add_(1)
+    with torch.cuda.graph(fixed):
+        same = step(step=first)
+    for k in range(5):
+        graph.replay()
+        fixed.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(p, q) for p, q in zip(out, eager[k])), k
+        assert all(torch.equal(p, q) for p, q in zip(same, eager[0])), k
+        mine = step(step=first, counter=counter)     # eager, with the counter as it now is
+        if k < 4:
+            assert all(torch.equal(p, q) for p, q in zip(mine, eager[k + 1])), k

@@ -105,3 +105,20 @@ def test_functions_refuse_tensors_whose_gradient_would_be_lost():
             f()
         with torch.no_grad(), pytest.raises(M.AuvError, match="on a GPU"):      # taken as far as the next check
             f()
+
+
+def test_dropout_counter_is_checked():
+    import paper_2512_13359_amd as M
+    from paper_2512_13359_amd import _abi as A
+    d = M.make_drop(0.5, 1)
+    assert d.counter is None and d.tensor is None
+    for bad in (torch.zeros(1, dtype=torch.int32), torch.zeros(1), torch.zeros(2, dtype=torch.int32)):     # on the host, too
+        with pytest.raises(M.AuvError, match="counter"):
+            M.make_drop(0.5, 1, counter=bad)
+    rows = A.AuvRows(P, 24, 8), None, A.AuvRows(2 * P, 24, 8)
+    odd = A.AuvDrop(1, 0, 0, 0, 10, P + 2)
+    assert A.lib.auv_dropout(odd, 0, 2, 3, 8, *rows, None) == A.AUV_EINVAL and "counter" in A.auv_last_error()
+    x = torch.zeros(4, 8)
+    for f in (lambda: M.dropout(x, 0.5), lambda: M.dropout(x, None), lambda: M.norm_forward(x, 2, drop=0.5)):
+        with pytest.raises(M.AuvError, match="make_drop"):
+            f()
