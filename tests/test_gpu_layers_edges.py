@@ -6,7 +6,7 @@ import torch
 
 from oracle import layers as L
 from tests.gpu_util import announce, host, require_gpu
-from tests.test_gpu_layers import HALF, TYPES, U, check_norm, f64, scan_inputs, seq, within
+from tests.test_gpu_layers import HALF, TYPES, U, block, block_setup, check_norm, f64, scan_inputs, seq, within
 
 pytestmark = pytest.mark.gpu
 
@@ -201,3 +201,26 @@ def test_captured_dropout_draws_by_its_counter(n, s, c, groups):
         mine = step(step=first, counter=counter)     # eager, with the counter as it now is
         if k < 4:
             assert all(torch.equal(p, q) for p, q in zip(mine, eager[k + 1])), k
+
+
+def test_block_replays_equal_the_calls_before_the_capture():
+    """Replays against results from before the capture, not only against eager calls beside them; and the refilled input counts."""
+    require_gpu()
+    T, n, c = 24, 65, 17
+    feat, done, P, dlast = block_setup(T, n, c)
+    want = {k: v.clone() for k, v in block(feat, done, P, 5, T, n, c, dlast).items()}
+    flip = {k: v.clone() for k, v in block(feat.flip(0).contiguous(), done, P, 5, T, n, c, dlast).items()}
+    f = feat.clone()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = block(f, done, P, 5, T, n, c, dlast)
+    for rep in range(5):
+        f.copy_(feat.flip(0) if rep % 2 else feat)
+        graph.replay()
+        block(feat, done, P, 6, T, n, c, dlast)     # the program's own work between
+        torch.cuda.synchronize()
+        for k, v in (flip if rep % 2 else want).items():
+            assert torch.equal(out[k], v), (rep, k)
+    # the two differ, but for the last state: episodes of 8 steps all end with step 24
+    assert (want["last"] == 0).all() and all(not torch.equal(want[k], flip[k]) for k in want if k != "last")
