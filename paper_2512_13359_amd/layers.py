@@ -163,7 +163,7 @@ def scan_backward(gate, x, h, *, dout=None, dh_last=None, kind="sigmoid", done=N
     dgate and dx have x's type (zero at held steps), or are the pair `out`: the halves of one
     buffer, say, where gate and x are the halves of one projection.  dh0 is float32 [n][c]."""
     fn = "scan_backward"
-    _unrecorded(fn, gate, x, h, dout, dh_last, h0, *(out or ()))
+    _unrecorded(fn, gate, x, h, dout, dh_last, h0, *(() if out is None else out))
     head = _scan(fn, gate, x, kind, done, lens, h0)
     _like(fn, "h", h, x.shape, x.dtype, x.get_device())
     if dout is not None:

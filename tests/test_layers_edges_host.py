@@ -122,3 +122,14 @@ def test_dropout_counter_is_checked():
     for f in (lambda: M.dropout(x, 0.5), lambda: M.dropout(x, None), lambda: M.norm_forward(x, 2, drop=0.5)):
         with pytest.raises(M.AuvError, match="make_drop"):
             f()
+
+
+def test_scan_backward_takes_both_results_as_one_tensor():
+    """`out` may be any pair: a tensor whose first axis has the two."""
+    import paper_2512_13359_amd as M
+    x = torch.zeros(4, 3, 8)
+    for out in (torch.zeros(2, 4, 3, 8), [x, x], (x, x)):
+        with pytest.raises(M.AuvError, match="on a GPU"):
+            M.scan_backward(x, x, x, out=out)
+    with pytest.raises(M.AuvError, match="pair"):
+        M.scan_backward(x, x, x, out=torch.zeros(3, 4, 3, 8))
