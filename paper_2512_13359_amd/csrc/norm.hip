@@ -29,7 +29,7 @@ __device__ __forceinline__ void grad_of(int act, const float* w, const float* b,
 // A workgroup holds `pack` samples at a time in registers, R vectors per thread: a thread keeps V channels and takes
 // every step-th position of its sample.  Sums go from threads to columns (channels of a sample) to groups through LDS.
 // Read and written once; bound by the chain of a pass (load, two sums of three barriers each, store) where samples are small:
-// 30000 x 8 x 32 bf16 in 8 groups, forward 18 us (1.7 TB/s) and backward 32; 20000 x 2000 fp32 79 (4.1) and 118 (4.1).
+// 30000 x 8 x 32 bf16 in 8 groups, forward 19 us (1.6 TB/s) and backward 34; 20000 x 2000 fp32 82 (3.9) and 119 (4.0).
 template <class T, int V, int R> struct BlockTeam {
   bool on;
   int c, shift, p, row, q;   // channel, sample of the pass, first position, row of LDS
@@ -318,8 +318,9 @@ __global__ __launch_bounds__(512) void k_norm_block_grad(NormArgs a) {
 // ------------------------------------------------------------------ chunk form -------
 // A workgroup walks over a chunk of a sample's positions and a tile of its channels, a thread keeping V channels.  The
 // first launch leaves every chunk's and tile's share of the statistics of the tile's groups, [n][chunk][tile][held]; the second
-// joins a group's shares in its first instructions.  Bound by HBM and the second read: 32 x 4096 x 256 bf16 in 32 groups with SiLU, 13 us for the
-// statistics (5.2 TB/s) and 26 for the rest (5.2); backward 68.
+// joins a group's shares in its first instructions.  Bound by HBM and the second read: 32 x 4096 x 256 bf16 in 32 groups with SiLU, 15 us for the
+// statistics (4.5 TB/s) and 26 for the rest (5.2); backward 70.  Samples of one position are far from it: 20000 rows of 4104 bf16
+// channels 554 us forward (0.6 TB/s) and 1110 backward (0.4).
 template <class T, int V> struct Walker {
   bool on;
   int i, chunk, c, shift, row, step, s0, s1;   // sample, chunk, channel, positions [s0, s1) from s0 + row on by `step`
@@ -748,8 +749,8 @@ __global__ __launch_bounds__(1024) void k_norm_param_sum(NormArgs a) {
 
 // -------------------------------------------------------------------- host side -------
 
-// Workgroups per CU, each for many rows: 262144 x 256 bf16 with SiLU, forward 8 per CU 52 us, 2 60, 32 70; backward 3 per CU 85
-// (with dropout 112), 2 80 (121), 8 92 (110).
+// Workgroups per CU, each for many rows: 262144 x 256 bf16 with SiLU (and dropout), forward 8 per CU 58 us (62), 2 65 (81), 32 77
+// (79); backward 3 per CU 89 (91), 2 87 (97), 8 91 (95).
 static bool plan_rows(const auv_norm* d, bool dense, bool backward, NormPlan& p) {
   const int full = d->type == AUV_BF16 ? 8 : 4;
   const int64_t m = (int64_t)d->s * (d->c / d->groups);
@@ -813,8 +814,8 @@ static size_t block_lds(const auv_norm* d, const NormPlan& p) {   // see the ker
 }
 
 // The block form's launch, by workgroups that are all resident: each keeps weights and sums over its samples, and one more
-// round of a few would last as long as all others (11803 x 8 x 160 fp32 in 32 groups, backward: 12 waves per CU, which the
-// registers hold, 78 us, 16 107).
+// round of a few would last as long as all others (11803 x 8 x 160 fp32 in 32 groups, tanh and dropout, backward: 12 waves per CU,
+// which the registers hold, 79 us, 16 109, 8 97).
 static int launch_block(const char* fn, const auv_norm* d, NormPlan& p, NormArgs& a, bool grad, hipStream_t s) {
   const bool bf16 = d->type == AUV_BF16, drop = d->drop && d->drop->drop, merged = a.Cg % p.V == 0;
   const void* k = !grad ? AUV_BLOCK_KERNEL(k_norm_block)

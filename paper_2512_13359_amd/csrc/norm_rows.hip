@@ -45,8 +45,8 @@ template <class T, int V, int NV> struct RowTeam {
   }
 };
 
-// Bound by HBM, x in and y out: 262144 x 256 bf16 with SiLU in 52 us (5.1 TB/s); with dropout in 59, where Philox's 18 quarter-rate
-// products per eight elements fill the VALU beside it.
+// Bound by HBM, x in and y out: 262144 x 256 bf16 with SiLU and dropout in 70 us (3.8 TB/s) between backward passes, in 62 alone
+// (without dropout 58, 4.7 TB/s): Philox's 18 quarter-rate products per eight elements fill the VALU beside it.
 template <class T, int V, int NV, bool DROP, bool FULL>
 __global__ __launch_bounds__(256) void k_norm_rows(NormArgs a) {
   if constexpr (DROP) a.drop.count();
@@ -126,7 +126,7 @@ __global__ __launch_bounds__(256) void k_norm_rows(NormArgs a) {
   }
 }
 
-// Bound by HBM, x and dy in and dx out: the same in 83 us with the parameters' sum (4.8 TB/s), with dropout 89.
+// Bound by HBM, x and dy in and dx out: the same in 86 us (4.7 TB/s); alone with the parameters' sum 91 (without dropout 89).
 template <class T, int V, int NV, bool DROP, bool FULL>
 __global__ __launch_bounds__(256) void k_norm_rows_grad(NormArgs a) {
   if constexpr (DROP) a.drop.count();

@@ -10,7 +10,7 @@
 namespace auv {
 
 // (P, S) of every chunk of steps but the last: each wave runs a contiguous part of its chunk, the
-// first wave joins the parts.  Reads gate and input once: 2 x 256 bf16 columns x 32768 steps in 13 us (5.2 TB/s).
+// first wave joins the parts.  Reads gate and input once: 2 x 256 bf16 columns x 32768 steps in 14 us (4.8 TB/s).
 template <class T, int V, bool SIG, bool MASK, bool NI>
 __global__ __launch_bounds__(64 * SCAN_WAVES) void k_scan_ranges(ScanArgs a) {
   constexpr int U = scan_steps<V>();
@@ -50,8 +50,8 @@ __global__ __launch_bounds__(64 * SCAN_WAVES) void k_scan_ranges(ScanArgs a) {
 }
 
 // The states: the waves' ranges joined round by round, each wave's steps redone from the true state with gate and input still
-// in registers.  Bound by HBM, three tensors once: 16384 x 64 bf16 columns x 64 steps in 72 us (5.6 TB/s), 4096 x 64 x 512
-// in 167 (4.8), 4095 x 23 fp32 x 500 with the sequence fastest, ends and lengths in 137 (4.1; aligned rows without them 106); below some
+// in registers.  Bound by HBM, three tensors once: 16384 x 64 bf16 columns x 64 steps in 73 us (5.5 TB/s), 4096 x 64 x 512
+// in 175 (4.6), 4095 x 23 fp32 x 500 with the sequence fastest, ends and lengths in 141 (4.0; aligned rows without them 106); below some
 // thousand columns by a round's chain (load, ranges through LDS, steps: about 1.5 us for 32 or 64 steps).
 template <class T, int V, bool SIG, bool MASK, bool NI>
 __global__ __launch_bounds__(64 * SCAN_WAVES) void k_scan_forward(ScanArgs a) {
@@ -245,9 +245,9 @@ static void scan_shape(const auv_scan* d, const auv_seq* const* seqs, int count,
   auto tiles_of = [&](int V) { return (int)(((int64_t)a.Lo * ((a.Li + V - 1) / V) + 63) / 64); };
   // A vector that straddles sequences straddles two at most.
   auto fits = [&](int V) { return unit && a.Li >= V && (sh.ni || c >= V || a.Li == c); };
-  // Wide vectors where they leave four waves per CU: bf16, 4096 x 64 columns x 512 steps, both directions: V = 4 in 495
-  // us, V = 2 535, V = 1 650, V = 8 (at its best, four waves per workgroup; more registers) 531.  Else two columns per lane: they make the
-  // fewest lane accesses that still fill the chip (37037 bf16 columns x 700: V = 4 in 204, V = 2 177, V = 1 209); but
+  // Wide vectors where they leave four waves per CU: bf16, 4096 x 64 columns x 512 steps, both directions: V = 4 in 595
+  // us, V = 2 640, V = 1 997.  Else two columns per lane: they make the fewest lane accesses that still fill the chip
+  // (37037 bf16 columns x 700: V = 4 in 199, V = 2 153, V = 1 146); but
   // one where only that gives a workgroup per CU without splitting the steps and an access is 4 bytes all the same
   // (fp32, 16384 columns x 1024: V = 1 in 142, V = 2 split in four 167).
   sh.V = fits(4) && tiles_of(4) >= 4 * cus ? 4 : fits(2) && tiles_of(1) > 1 ? 2 : 1;
@@ -256,8 +256,8 @@ static void scan_shape(const auv_scan* d, const auv_seq* const* seqs, int count,
   a.tiles = tiles_of(sh.V);
   const int U = sh.steps = sh.V >= (grad ? 2 : 4) ? 4 : 8;   // scan_steps, scan_grad_steps
   // Waves per workgroup until there are eight per CU (4095 x 23 fp32 columns x 500 steps, 736 tiles, forward and backward: one wave
-  // 160 and 355 us, two 145 and 260, four 142 and 243; where there are eight anyway one wave is best, 16384 x 64 columns x 64 steps: 81, two
-  // waves 88); four per CU do for accesses of 16 bytes (4096 x 64 fp32 columns x 128: one wave 73 and 149, two 79 and 157).
+  // 160 and 355 us, two 145 and 260, four 142 and 243; where there are eight anyway one wave is best, 16384 x 64 bf16 columns x 64 steps
+  // forward: 74, two waves 87); four per CU do for accesses of 16 bytes (4096 x 64 fp32 columns x 128: one wave 73 and 149, two 79 and 157).
   // A bf16 gradient leaves the state before each round: rounds of 8 steps at least (a quarter of a tensor in the workspace, or
   // 16 KB of LDS; backward of 16384 x 64 columns x 64 steps: 4 steps 215 us, 8 187, 16 194; 4096 x 64 x 512: 8 411, 16 495).
   sh.W = 1;
@@ -265,9 +265,10 @@ static void scan_shape(const auv_scan* d, const auv_seq* const* seqs, int count,
   const int enough = sh.V == 4 && d->type == AUV_FP32 ? 4 : 8;
   while (sh.W < SCAN_WAVES && sh.W * U < d->T && ((int64_t)a.tiles * sh.W < enough * cus || (marks && sh.W * U < 8))) sh.W *= 2;
   const int span = sh.W * U, rounds = (d->T - 1) / span + 1;
-  // Steps split over workgroups where there is less than one per CU, up to two per CU: reads gate and input (or dout) twice.
-  // 2048 columns x 4096 steps: whole 201 and 398 us, split in 16 30 and 43, in 32 25 and 33; 16384 columns x 1024 steps: whole 54 and
-  // 105, in four 39 and 54, in eight 46 and 59; 32768 columns (256 tiles): whole 57 and 115, in two 64 and 107.
+  // Steps split over workgroups where there is less than one per CU, up to two per CU: reads gate and input (or dout) once more.
+  // bf16, forward and backward: 2048 columns x 4096 steps whole 147 and 470 us, split in 16 23 and 55, in 32 21 and 44, in 64 26 and 51;
+  // 16384 columns x 1024 steps whole 41 and 122, in four 33 and 70, in eight 37 and 73; 32768 columns (256 tiles) whole 43 and 123, in
+  // two 51 and 114.
   sh.K = 1;
   const bool in_place = d->last.p && d->last.p == d->h0.p;   // its chunks would read what the last one writes
   if (sh.W == SCAN_WAVES && rounds >= 4 && d->T >= AUV_SCAN_SPLIT_STEPS && a.tiles < cus && !in_place)
@@ -277,7 +278,7 @@ static void scan_shape(const auv_scan* d, const auv_seq* const* seqs, int count,
   a.K = sh.K;
   a.grouped = sh.K == 1 && d->x.st * (d->type == AUV_BF16 ? 2 : 4) % 128 != 0;
   // Stores pass by the caches (16384 x 64 bf16 columns x 64 steps: 81 us without the hint, 72 with it), but for fp32 rows that share
-  // lines (4095 x 23 columns x 500 steps, forward and backward 359 us plain, 375 with it; bf16, 37037 columns x 700 steps: 168 plain, 147).
+  // lines (4095 x 23 columns x 500 steps, forward and backward 359 us plain, 375 with it; bf16, 37037 columns x 700 steps: 158 plain, 159).
   a.shared = a.grouped && d->type == AUV_FP32;
   a.T = d->T;
   a.n = n;

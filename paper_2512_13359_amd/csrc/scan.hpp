@@ -59,8 +59,8 @@ __device__ __forceinline__ float after(float P, float S, float s) { return P == 
 
 // A workgroup's tile of columns and chunk of steps.  Where rows do not start at a cache line, neighbouring tiles go to one
 // XCD (workgroups are dealt out to the eight in turn), so that the parts of a line that two tiles share meet in one L2:
-// 4095 x 23 fp32 columns x 500 steps, forward and backward 382 -> 358 us.  Aligned rows share none and run faster dealt out
-// (16384 x 64 bf16 columns x 64 steps 81 us, grouped 86), and so do chunks of steps (2 x 256 x 32768: 85, grouped 92).
+// 4095 x 23 fp32 columns x 500 steps, forward and backward 382 -> 358 us.  Aligned rows share none (16384 x 64 bf16 columns x
+// 64 steps, forward 75 us, grouped 73), and chunks of steps run faster dealt out (2 x 256 x 32768, forward and backward 111, grouped 120).
 struct Place {
   int tile, chunk;
   __device__ __forceinline__ explicit Place(const ScanArgs& a) {

@@ -176,7 +176,7 @@ template <int V> struct Marks {
 // The gradients, rounds and waves from the last step to the first.  bf16: a walk from the first step to the last before it
 // leaves the state before each round, and a round forms its states from there.  Bound by HBM, gate, input, output (bf16: gate and
 // input a second time, a quarter of a tensor out and in) and its gradient in, two gradients out: 4096 x 64 bf16 columns x 512 steps
-// in 411 us (4.9 TB/s; with the states read from h 326), 4095 x 23 fp32 x 500 with ends and lengths in 225 (4.2).
+// in 432 us (4.7 TB/s; with the states read from h 338), 4095 x 23 fp32 x 500 with ends and lengths in 222 (4.3).
 template <class T, int V, bool SIG, bool MASK, bool NI>
 __global__ __launch_bounds__(64 * SCAN_WAVES) void k_scan_backward(ScanArgs a) {
   constexpr int U = scan_grad_steps<V>();
