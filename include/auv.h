@@ -544,8 +544,9 @@ typedef struct {
   uint32_t site;  /* layer, below 2^24 */
   uint32_t row0;
   uint32_t drop;  /* probability in 65536ths, below 65536 */
-  const uint32_t* counter; /* one word of device memory that is added to step (modulo 2^32) when the call runs, or NULL; with
-                              it a call captured into a graph draws anew at each replay, else the same elements every time */
+  const uint32_t* counter; /* one word of device memory that is added to step (modulo 2^32) when the call runs, or NULL: a call
+                              captured into a graph draws the same elements at every replay unless the word has changed.  The
+                              same value is to be there forward and backward */
 } auv_drop;
 
 /* Channels-last tensor [n][s][c] of stride 1 over c: row (i, j) starts at p + i sn + j ss.  Rows are

@@ -443,7 +443,8 @@ def make_drop(p: float, seed: int, step: int = 0, site: int = 0, row0: int = 0, 
     """Dropout with probability p (rounded to 65536ths): the draws of update `step` and layer `site`
     (below 2^24) under a 64-bit seed; row0: global number of the tensors' first row.  counter: an int32
     tensor of one element on the GPU, added to step when a call runs.  A call captured into a graph draws the
-    same elements at every replay unless a counter that the program advances tells them apart."""
+    same elements at every replay unless a counter tells them apart, which the program advances once per replay,
+    after the backward pass that draws the forward pass's mask again."""
     if not 0.0 <= p < 1.0 or round(p * 65536) >= 65536:
         raise AuvError(AUV_EINVAL, f"make_drop: p must be in [0, 1) and below 1 in 65536ths, got {p}")
     for name, v, bits in (("seed", seed, 64), ("step", step, 32), ("site", site, 24), ("row0", row0, 32)):

@@ -557,7 +557,7 @@ __global__ __launch_bounds__(256) void k_norm_apply(NormArgs a) {
 }
 
 // MANY: a workgroup takes every `slots`-th sample and keeps the sums of the parameters' gradients over them in registers, so that
-// 65536 rows of 8192 bf16 channels leave 256 partial rows (17 MB), not one each.
+// 65536 rows of 8192 bf16 channels leave 192 partial rows (13 MB), not one each.
 template <class T, int V, bool DROP, bool MANY>
 __global__ __launch_bounds__(256) void k_norm_grad_sums(NormArgs a) {
   if constexpr (DROP) a.drop.count();
