@@ -514,7 +514,7 @@ typedef struct {
                            fp32 from gate, x, done, lens and h0 instead of taking them from there */
   const float* done;    /* [T][n] as auv_rollout records it, or NULL */
   const int32_t* lens;  /* [n] steps of each sequence, below 0 as 0, above T as T; or NULL */
-  auv_seq_state h0;     /* p NULL: zero */
+  auv_seq_state h0;     /* p NULL: zero; backward: as it was before the forward pass */
   auv_seq_state last;   /* forward: s_{T-1}, or p NULL; may be the memory of h0 with the same strides */
 } auv_scan;
 
